@@ -406,6 +406,48 @@ size_t dp_conv_workspace_bytes(dp_op op, int64_t B, int64_t H, int64_t W, int64_
 int dp_conv_rows_resident(int64_t B, int64_t H, int64_t W, int64_t C,
                           int64_t KH, int64_t KW, int64_t pad, int64_t d_out, dp_dtype dtype);
 
+/* The norm of a gradient that consists of many tensors, and the same tensors
+ * scaled by the clip factor of that norm (the clip function of Section 3.2 on a
+ * whole gradient: a micro-batch's or a user's before it joins the private sum,
+ * the finished one of a step, or training without privacy):
+ *     norm   = sqrt( (accumulate ? norm^2 : 0) + sum_l sum_j x_l[j]^2 )
+ *     out_l  = (accumulate ? out_l : 0) + 1 / max(1, norm / C) * x_l
+ * Squares and sums are taken in 64 bits, so neither overflows nor vanishes for any
+ * float32 input, and `norm` is rounded to float32 once.  A NaN or an infinity in
+ * any tensor makes the norm NaN or infinite; the factor is then NaN or 0.
+ * The tensors of a call may differ in type and size. */
+typedef struct {
+    const void* x;       /* device, n elements of `dtype` one after the other, aligned to one element; NULL if n == 0 */
+    void* out;           /* dp_tensors_clip and dp_tensors_norm_clip: device, n elements of `out_dtype`; x itself (then
+                            out_dtype == dtype), or memory that no x and no other out of the call shares */
+    int64_t n;
+    dp_dtype dtype;      /* DP_F32, DP_BF16 or DP_F16; 8-bit types give DP_ERR_UNSUPPORTED */
+    dp_dtype out_dtype;  /* dtype or DP_F32; DP_F32 if the call accumulates */
+} dp_tensor_desc;
+
+/*   tensors       HOST array, read during the call only; at most 2^20 descriptors and 2^48 elements in all
+ *   norm          device float32[1], written (read first if accumulate)
+ *   tensor_norms  NULL, or device float32[n_tensors]: the norm of each tensor by itself
+ *   workspace     device scratch of at least dp_tensors_workspace_bytes(n_tensors) bytes, 16-byte aligned */
+dp_status dp_tensors_norm(const dp_tensor_desc* tensors, int64_t n_tensors, int accumulate,
+                          float* norm, float* tensor_norms,
+                          void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* out_l = (accumulate ? out_l : 0) + 1 / max(1, norm / C) * x_l with a norm that is on
+ * the device already (one that dp_tensors_norm has taken, or that several processes
+ * have added up).  C > 0. */
+dp_status dp_tensors_clip(const dp_tensor_desc* tensors, int64_t n_tensors, const float* norm, float C,
+                          int accumulate, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Both in one call: dp_tensors_norm without accumulating, then dp_tensors_clip, with
+ * bit-identical results and fewer launches.  `accumulate` is that of the outputs. */
+dp_status dp_tensors_norm_clip(const dp_tensor_desc* tensors, int64_t n_tensors, float C, int accumulate,
+                               float* norm, float* tensor_norms,
+                               void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Scratch bytes for the three calls above; 0 for a number of tensors that they refuse. */
+size_t dp_tensors_workspace_bytes(int64_t n_tensors);
+
 /* Gaussian mechanism (Section 2, Gaussian-mechanism lemma; Algorithm 1, the
  * update line): grad[j] += stddev * z[offset + j], j in [0, n), with z an
  * i.i.d. N(0,1) stream that is a pure function of (seed, element index):

@@ -90,6 +90,17 @@ struct ClippedBiasDesc { const float* u; const float* clip; int D; float* grad_b
 hipError_t launch_clipped_bias_layers(const ClippedBiasDesc* layers, int n_layers, int B, bool accumulate, float stddev, uint64_t seed, hipStream_t st);
 hipError_t launch_philox_raw(uint32_t* out, int64_t n_counters, uint64_t seed, uint64_t first, hipStream_t st);
 
+// ---- norm and clipping of a gradient of many tensors (dp_tensors.hip)
+struct TensorItem { const void* x; void* out; int64_t n; int first_chunk; short dt, odt; };      // types as above
+constexpr int kTensorChunk = 4096;     // elements of the smallest chunk
+constexpr int kTensorChunks = 2048;    // chunks that a large set is cut into (one more at most for each tensor)
+int64_t tensor_chunk_elems(int64_t total);
+size_t tensors_ws_bytes(int64_t n_tensors);
+// first_chunk of every item is set (the items have at least one chunk each), `chunks` their number; norm != nullptr: take it
+hipError_t launch_tensors_norm(const TensorItem* items, int n, int64_t chunk, int chunks, bool accumulate, float* norm, float* tensor_norms, void* ws, hipStream_t st);
+hipError_t launch_tensors_clip(const TensorItem* items, int n, int64_t chunk, int chunks, bool accumulate, const float* norm, float C, void* ws, hipStream_t st);
+hipError_t launch_tensors_norm_clip(const TensorItem* items, int n, int64_t chunk, int chunks, bool accumulate, float* norm, float* tensor_norms, float C, void* ws, hipStream_t st);
+
 // ---- K-major ("TN") products  sum_k A[k,:]^T G[k,:]  (dp_tn_bf16.hip, dp_tn_f32.hip)
 struct TnPlan {
     int tile_m, tile_n;     // block tile

@@ -1,0 +1,249 @@
+// Norm and clipping of a gradient of many tensors:  norm = sqrt(sum_l sum_j x_l[j]^2),
+//     out_l = (accumulate ? out_l : 0) + 1 / max(1, norm / C) * x_l.
+// Bound by memory: the norm has to be known before the first product, so x is read twice (the second time out of the
+// last-level cache where the set fits it) and out is written once.
+//
+// The tensors are cut into chunks of one size, a workgroup each; the sum of a chunk's squares is one double of the
+// workspace.  Squares and sums are doubles: a square of any float32 is exact and in range there, and their two
+// instructions per element stay behind the loads.  The order of the additions is fixed.
+#include <algorithm>
+#include "dp_elems.h"
+#include "dp_internal.h"
+
+namespace dpk {
+
+namespace {
+
+// Descriptors travel as kernel arguments, whose block holds 4 KB; longer lists are written to the head of the
+// workspace by small launches first.
+constexpr int kDirectItems = 112;
+struct ItemTable { TensorItem items[kDirectItems]; };
+
+__global__ __launch_bounds__(128) void k_tensors_table(ItemTable t, int n, TensorItem* __restrict__ out) {
+    if ((int)threadIdx.x < n) out[threadIdx.x] = t.items[threadIdx.x];
+}
+
+// the item that chunk c belongs to: the last one that begins at c or before; 256 candidates at a time
+__device__ __forceinline__ int find_item(const TensorItem* __restrict__ items, int n, int c) {
+    int lo = 0, len = n;
+    while (len > 1) {
+        const int step = (len + kThreads - 1) / kThreads;
+        const int k = (int)threadIdx.x * step;
+        const int before = __syncthreads_count(k < len && items[lo + k].first_chunk <= c);      // at least 1: lo itself
+        const int skip = (before - 1) * step;
+        lo += skip;
+        len = min(step, len - skip);
+    }
+    return __builtin_amdgcn_readfirstlane(lo);
+}
+
+template <int DT> __device__ __forceinline__ double sum_squares(const void* __restrict__ x, int64_t begin, int64_t end) {
+    double acc[4] = {0.0, 0.0, 0.0, 0.0};
+    auto add = [&](const Raw8<DT>& r) {
+        float v[8];
+        widen8<DT>(r, v);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) { const double d = v[j]; acc[j & 3] = fma(d, d, acc[j & 3]); }
+    };
+    int64_t k = begin + (int64_t)threadIdx.x * 8;
+    for (; k + 3 * 8 * kThreads + 8 <= end; k += 4 * 8 * kThreads) {       // four loads in flight
+        Raw8<DT> r[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = load_raw8<DT>(x, k + i * 8 * kThreads);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) add(r[i]);
+    }
+    for (; k + 8 <= end; k += 8 * kThreads) add(load_raw8<DT>(x, k));
+    for (; k < end; ++k) { const double d = load_one<DT>(x, k); acc[0] = fma(d, d, acc[0]); }      // the last elements: one thread's
+    return (acc[0] + acc[1]) + (acc[2] + acc[3]);
+}
+
+template <bool DIRECT>
+__global__ __launch_bounds__(kThreads) void k_tensors_squares(ItemTable t, const TensorItem* __restrict__ table, int n, int64_t chunk, double* __restrict__ partial) {
+    __shared__ double red[4];
+    const TensorItem* items = DIRECT ? t.items : table;
+    const int c = blockIdx.x, i = find_item(items, n, c);
+    const int64_t begin = (int64_t)(c - items[i].first_chunk) * chunk, end = min(items[i].n, begin + chunk);
+    const void* x = items[i].x;
+    double s = 0.0;
+    switch (items[i].dt) {
+    case 0: s = sum_squares<0>(x, begin, end); break;
+    case 1: s = sum_squares<1>(x, begin, end); break;
+    default: s = sum_squares<2>(x, begin, end); break;
+    }
+    s = block_sum_256_f64(s, red);
+    if (threadIdx.x == 0) partial[c] = s;
+}
+
+// the sum of all chunks, by every workgroup that asks in the same order
+__device__ __forceinline__ double sum_partials(const double* __restrict__ partial, int chunks, double* red) {
+    double s = 0.0;
+    int c = threadIdx.x;
+    for (; c + 7 * kThreads < chunks; c += 8 * kThreads) {
+        double v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = partial[c + k * kThreads];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s += v[k];
+    }
+    for (; c < chunks; c += kThreads) s += partial[c];
+    return block_sum_256_f64(s, red);
+}
+
+// norms of the tensors by themselves: a wave adds up an item's chunks
+__device__ __forceinline__ void item_norm(const double* __restrict__ partial, int first, int last, float* out) {
+    double s = 0.0;
+    for (int c = first + (threadIdx.x & (kWave - 1)); c < last; c += kWave) s += partial[c];
+    s = wave_sum_f64(s);
+    if ((threadIdx.x & (kWave - 1)) == 0) *out = (float)sqrt(s);
+}
+
+// workgroup 0: the norm; the others: the norms of four tensors each
+template <bool DIRECT>
+__global__ __launch_bounds__(kThreads) void k_tensors_fold(ItemTable t, const TensorItem* __restrict__ table, int n, int chunks, const double* __restrict__ partial,
+                                                           int accumulate, float* __restrict__ norm, float* __restrict__ tensor_norms) {
+    __shared__ double red[4];
+    const TensorItem* items = DIRECT ? t.items : table;
+    if (blockIdx.x == 0) {
+        double s = sum_partials(partial, chunks, red);
+        if (threadIdx.x == 0) {
+            if (accumulate) { const double old = norm[0]; s += old * old; }
+            norm[0] = (float)sqrt(s);
+        }
+        return;
+    }
+    const int i = (blockIdx.x - 1) * (kThreads / kWave) + (threadIdx.x >> 6);
+    if (i < n) item_norm(partial, items[i].first_chunk, i + 1 < n ? items[i + 1].first_chunk : chunks, tensor_norms + i);
+}
+
+template <int DT, int ODT> __device__ __forceinline__ void scale(const void* x, void* out, int64_t begin, int64_t end, float f, bool accumulate) {
+    int64_t k = begin + (int64_t)threadIdx.x * 8;
+    for (; k + 8 <= end; k += 8 * kThreads) {
+        float v[8];
+        load8<DT>(x, k, v);
+        if (accumulate) {
+            float o[8];
+            load8<ODT>(out, k, o);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = o[j] + f * v[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= f;
+        }
+        store8<ODT>(out, k, v);
+    }
+    for (; k < end; ++k) {
+        const float v = f * load_one<DT>(x, k);
+        store_one<ODT>(out, k, accumulate ? load_one<ODT>(out, k) + v : v);
+    }
+}
+
+// partial != nullptr: the norm is taken from the chunks' sums by every workgroup for itself, and written
+template <bool DIRECT>
+__global__ __launch_bounds__(kThreads) void k_tensors_scale(ItemTable t, const TensorItem* __restrict__ table, int n, int64_t chunk, int chunks, int accumulate,
+                                                            const double* __restrict__ partial, float* __restrict__ norm, float* __restrict__ tensor_norms, float C) {
+    __shared__ double red[4];
+    const TensorItem* items = DIRECT ? t.items : table;
+    const int c = blockIdx.x, i = find_item(items, n, c);
+    float total;
+    if (partial) {
+        total = (float)sqrt(sum_partials(partial, chunks, red));
+        if (c == 0 && threadIdx.x == 0) norm[0] = total;
+        if (tensor_norms && c == items[i].first_chunk && threadIdx.x < kWave)
+            item_norm(partial, c, i + 1 < n ? items[i + 1].first_chunk : chunks, tensor_norms + i);
+    } else {
+        total = norm[0];
+    }
+    const float m = total / C, f = 1.0f / (!(m <= 1.0f) ? m : 1.0f);       // the max lets a NaN norm through
+    const int64_t begin = (int64_t)(c - items[i].first_chunk) * chunk, end = min(items[i].n, begin + chunk);
+    const void* x = items[i].x;
+    void* out = items[i].out;
+    if (f == 1.0f && x == out && !accumulate) return;                      // a factor of 1 leaves every value as it is
+    switch (items[i].dt * 4 + items[i].odt) {
+    case 0: scale<0, 0>(x, out, begin, end, f, accumulate); break;
+    case 4: scale<1, 0>(x, out, begin, end, f, accumulate); break;
+    case 5: scale<1, 1>(x, out, begin, end, f, false); break;
+    case 8: scale<2, 0>(x, out, begin, end, f, accumulate); break;
+    default: scale<2, 2>(x, out, begin, end, f, false); break;
+    }
+}
+
+// Workspace: the table of items that do not fit the arguments, then the chunks' sums.
+size_t table_bytes(int64_t n) { return n > kDirectItems ? (size_t)n * sizeof(TensorItem) : 0; }
+
+struct Tables { ItemTable args; const TensorItem* table = nullptr; double* partial = nullptr; };
+hipError_t place_items(const TensorItem* items, int n, void* ws, hipStream_t st, Tables& t) {
+    t.partial = reinterpret_cast<double*>(static_cast<unsigned char*>(ws) + table_bytes(n));
+    if (n <= kDirectItems) {
+        std::copy(items, items + n, t.args.items);
+        return hipSuccess;
+    }
+    TensorItem* to = static_cast<TensorItem*>(ws);
+    t.table = to;
+    for (int at = 0; at < n; at += kDirectItems) {
+        const int m = std::min(n - at, kDirectItems);
+        std::copy(items + at, items + at + m, t.args.items);
+        k_tensors_table<<<1, 128, 0, st>>>(t.args, m, to + at);
+    }
+    return hipGetLastError();
+}
+
+// Up to here every workgroup of the scaling launch adds up the chunks' sums by itself
+constexpr int kOwnFold = 4096;
+
+void squares(const Tables& t, int n, int64_t chunk, int chunks, hipStream_t st) {
+    if (t.table) k_tensors_squares<false><<<chunks, kThreads, 0, st>>>(t.args, t.table, n, chunk, t.partial);
+    else         k_tensors_squares<true><<<chunks, kThreads, 0, st>>>(t.args, nullptr, n, chunk, t.partial);
+}
+void fold(const Tables& t, int n, int chunks, bool accumulate, float* norm, float* tensor_norms, hipStream_t st) {
+    const int grid = 1 + (tensor_norms ? ceil_div(n, kThreads / kWave) : 0);
+    if (t.table) k_tensors_fold<false><<<grid, kThreads, 0, st>>>(t.args, t.table, n, chunks, t.partial, accumulate, norm, tensor_norms);
+    else         k_tensors_fold<true><<<grid, kThreads, 0, st>>>(t.args, nullptr, n, chunks, t.partial, accumulate, norm, tensor_norms);
+}
+void scaled(const Tables& t, int n, int64_t chunk, int chunks, bool accumulate, const double* partial, float* norm, float* tensor_norms, float C, hipStream_t st) {
+    if (t.table) k_tensors_scale<false><<<chunks, kThreads, 0, st>>>(t.args, t.table, n, chunk, chunks, accumulate, partial, norm, tensor_norms, C);
+    else         k_tensors_scale<true><<<chunks, kThreads, 0, st>>>(t.args, nullptr, n, chunk, chunks, accumulate, partial, norm, tensor_norms, C);
+}
+
+}  // namespace
+
+// Chunks of at least 4096 elements (two 16-byte pieces of float32 for every thread), and larger ones where that makes more than
+// 2048 of them (eight workgroups for each of the 256 compute units).
+int64_t tensor_chunk_elems(int64_t total) {
+    const int64_t unit = 8 * kThreads;
+    return std::max<int64_t>(kTensorChunk, (total / kTensorChunks + unit) / unit * unit);
+}
+size_t tensors_ws_bytes(int64_t n_tensors) {
+    return table_bytes(n_tensors) + (size_t)(kTensorChunks + n_tensors + 1) * sizeof(double);
+}
+
+hipError_t launch_tensors_norm(const TensorItem* items, int n, int64_t chunk, int chunks, bool accumulate, float* norm, float* tensor_norms, void* ws, hipStream_t st) {
+    Tables t;
+    const hipError_t e = place_items(items, n, ws, st, t);
+    if (e != hipSuccess) return e;
+    squares(t, n, chunk, chunks, st);
+    fold(t, n, chunks, accumulate, norm, tensor_norms, st);
+    return hipGetLastError();
+}
+hipError_t launch_tensors_clip(const TensorItem* items, int n, int64_t chunk, int chunks, bool accumulate, const float* norm, float C, void* ws, hipStream_t st) {
+    Tables t;
+    const hipError_t e = place_items(items, n, ws, st, t);
+    if (e != hipSuccess) return e;
+    scaled(t, n, chunk, chunks, accumulate, nullptr, const_cast<float*>(norm), nullptr, C, st);
+    return hipGetLastError();
+}
+hipError_t launch_tensors_norm_clip(const TensorItem* items, int n, int64_t chunk, int chunks, bool accumulate, float* norm, float* tensor_norms, float C, void* ws, hipStream_t st) {
+    Tables t;
+    const hipError_t e = place_items(items, n, ws, st, t);
+    if (e != hipSuccess) return e;
+    squares(t, n, chunk, chunks, st);
+    if (chunks > kOwnFold) {
+        fold(t, n, chunks, false, norm, tensor_norms, st);
+        scaled(t, n, chunk, chunks, accumulate, nullptr, norm, nullptr, C, st);
+    } else {
+        scaled(t, n, chunk, chunks, accumulate, t.partial, norm, tensor_norms, C, st);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace dpk

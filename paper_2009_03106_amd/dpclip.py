@@ -6,9 +6,10 @@ is no CPU fallback: if the library has not been built, loading raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
-from typing import Optional
+from typing import NamedTuple, Optional
 
 import torch
 
@@ -25,7 +26,7 @@ _PATHS = {"auto": DP_PATH_AUTO, "gram": DP_PATH_GRAM, "direct": DP_PATH_DIRECT}
 EXPORTS = ("dp_layer_sqnorm", "dp_layer_sqnorm_static", "dp_layers_sqnorm", "dp_layers_sqnorm_clip", "dp_layers_workspace_bytes", "dp_layers_clipped_grad",
            "dp_layers_clipped_grad_noise", "dp_layers_step", "dp_layers_clipped_workspace_bytes", "dp_clip_factors", "dp_clipped_grad", "dp_bias_sqnorm", "dp_clipped_bias_grad", "dp_layernorm_sqnorm",
            "dp_conv_sqnorm", "dp_conv_clipped_grad", "dp_conv_workspace_bytes", "dp_conv_rows_resident", "dp_add_noise", "dp_workspace_bytes", "dp_choose_path", "dp_status_string", "dp_philox_raw",
-           "dp_clipped_grad_rounds_inputs")
+           "dp_clipped_grad_rounds_inputs", "dp_tensors_norm", "dp_tensors_clip", "dp_tensors_norm_clip", "dp_tensors_workspace_bytes")
 
 # the measurement probes and plan queries of include/dpclip_probes.h
 PROBE_EXPORTS = ("dp_probe_mfma", "dp_probe_read", "dp_probe_lds_read", "dp_plan_gram_wide", "dp_plan_sums_in_two_lengths")
@@ -40,6 +41,12 @@ class LayerDesc(ctypes.Structure):
                 ("d_out", ctypes.c_int64), ("grad", ctypes.c_void_p), ("noise_offset", ctypes.c_uint64),
                 ("bias_rows", ctypes.c_void_p), ("sqnorm", ctypes.c_void_p), ("clip", ctypes.c_void_p),
                 ("clip_C", ctypes.c_float), ("grad_b", ctypes.c_void_p), ("bias_noise_offset", ctypes.c_uint64)]
+
+
+class TensorDesc(ctypes.Structure):
+    """dp_tensor_desc of the header."""
+    _fields_ = [("x", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int),
+                ("out_dtype", ctypes.c_int)]
 
 
 class DpclipError(RuntimeError):
@@ -107,6 +114,14 @@ def load_library() -> ctypes.CDLL:
     lib.dp_philox_raw.restype = ci
     lib.dp_clipped_grad_rounds_inputs.argtypes = [i64, i64, i64, i64, ci]
     lib.dp_clipped_grad_rounds_inputs.restype = ci
+    lib.dp_tensors_norm.argtypes = [ctypes.POINTER(TensorDesc), i64, ci, vp, vp, vp, sz, vp]
+    lib.dp_tensors_norm.restype = ci
+    lib.dp_tensors_clip.argtypes = [ctypes.POINTER(TensorDesc), i64, vp, f32, ci, vp, sz, vp]
+    lib.dp_tensors_clip.restype = ci
+    lib.dp_tensors_norm_clip.argtypes = [ctypes.POINTER(TensorDesc), i64, f32, ci, vp, vp, vp, sz, vp]
+    lib.dp_tensors_norm_clip.restype = ci
+    lib.dp_tensors_workspace_bytes.argtypes = [i64]
+    lib.dp_tensors_workspace_bytes.restype = sz
     lib.dp_probe_mfma.argtypes = [ci, ci, i64, vp, ctypes.POINTER(ctypes.c_double), vp]
     lib.dp_probe_mfma.restype = ci
     lib.dp_probe_read.argtypes = [vp, sz, vp, vp]
@@ -598,6 +613,134 @@ def add_noise(grad: torch.Tensor, stddev: float, seed: int, offset: int = 0, *,
                           _stream_ptr(stream))
     _check(st, "dp_add_noise")
     return grad
+
+
+def _here(device: torch.device, stream: Optional[torch.cuda.Stream], *tensors) -> None:
+    """The kernels run on the current device: every tensor, and the stream, has to belong to it."""
+    if device.type != "cuda":
+        raise ValueError("tensors must be contiguous device tensors")
+    if device.index != torch.cuda.current_device() or (stream is not None and stream.device.index != device.index):
+        raise ValueError(f"tensors and stream must be on the current device, not on {device}")
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError(f"tensors are on {device} and on {t.device}")
+
+
+def _made_on(stream: Optional[torch.cuda.Stream]):
+    """Where this module allocates for a call: on the call's own stream, whose earlier work the allocator knows."""
+    return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
+
+
+def _ws_args(ws: Optional[torch.Tensor]):
+    return (None, 0) if ws is None else (_ptr(ws), ws.numel() * ws.element_size())
+
+
+class TensorDescs(NamedTuple):
+    arr: object                     # ctypes array of dp_tensor_desc
+    device: torch.device
+    outs: Optional[list]            # the outputs, where the descriptors name any
+
+
+def tensor_descs(tensors, outs=None, *, in_place: bool = False) -> TensorDescs:
+    """Descriptors of contiguous float32, bfloat16 or float16 device tensors for the tensors_* calls, and of their
+    outputs: one per tensor, of its type or float32 and of its number of elements; with in_place the tensors
+    themselves.  Neither need be aligned to more than an element.  The tensors must stay alive, and where they are,
+    while the descriptors are used."""
+    tensors = list(tensors)
+    if in_place:
+        if outs is not None:
+            raise ValueError("outs or in_place, not both")
+        outs = tensors
+    outs = None if outs is None else list(outs)
+    if outs is not None and len(outs) != len(tensors):
+        raise ValueError("one output per tensor")
+    if not tensors:
+        raise ValueError("no tensors")
+    device = tensors[0].device
+    arr = (TensorDesc * len(tensors))()
+    for i, x in enumerate(tensors):
+        o = None if outs is None else outs[i]
+        for t in (x, o):
+            if t is not None and (t.device != device or not t.is_cuda or not t.is_contiguous()):
+                raise ValueError("tensors must be contiguous device tensors, all on one device")
+        code, ocode = _dtype_code(x), 0
+        if code > DP_F16:
+            raise TypeError(f"unsupported dtype {x.dtype}")
+        if o is not None:
+            if o.numel() != x.numel():
+                raise ValueError("an output must have as many elements as its tensor")
+            if o.dtype not in (x.dtype, torch.float32):
+                raise TypeError("an output must be of its tensor's dtype or float32")
+            ocode = _dtype_code(o)
+        arr[i] = TensorDesc(x.data_ptr() if x.numel() else None, o.data_ptr() if o is not None and x.numel() else None,
+                            x.numel(), code, ocode)
+    return TensorDescs(arr, device, outs)
+
+
+def tensors_workspace_bytes(descs: TensorDescs) -> int:
+    return int(load_library().dp_tensors_workspace_bytes(len(descs.arr)))
+
+
+def tensors_norm(tensors, norm: Optional[torch.Tensor] = None, *, accumulate: bool = False,
+                 tensor_norms: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                 descs: Optional[TensorDescs] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """norm[0] = sqrt((norm[0]^2 if accumulate) + sum of all elements' squares) via dp_tensors_norm; tensor_norms, a float32
+    tensor with an element per tensor, receives each one's own norm.  descs: the result of tensor_descs(tensors)."""
+    lib = load_library()
+    descs = descs if descs is not None else tensor_descs(tensors)
+    n = len(descs.arr)
+    if norm is None and accumulate:
+        raise ValueError("accumulate needs an existing norm tensor")
+    _here(descs.device, stream, norm, tensor_norms, workspace)
+    with _made_on(stream):
+        if norm is None:
+            norm = torch.empty(1, dtype=torch.float32, device=descs.device)
+        ws = _workspace(lambda: tensors_workspace_bytes(descs), descs.device, workspace)
+    st = lib.dp_tensors_norm(descs.arr, n, int(bool(accumulate)), _f32(norm, (1,), "norm"), _f32(tensor_norms, (n,), "tensor_norms"),
+                             *_ws_args(ws), _stream_ptr(stream))
+    _check(st, "dp_tensors_norm")
+    return norm
+
+
+def tensors_clip(tensors, norm: torch.Tensor, C: float, outs=None, *, accumulate: bool = False,
+                 workspace: Optional[torch.Tensor] = None, descs: Optional[TensorDescs] = None,
+                 stream: Optional[torch.cuda.Stream] = None):
+    """outs[l] = (outs[l] if accumulate) + min(1, C / norm[0]) * tensors[l] via dp_tensors_clip; in place without outs.
+    Accumulating takes float32 outs.  descs: the result of tensor_descs(tensors, outs).  Returns the outputs."""
+    lib = load_library()
+    if descs is None:
+        if accumulate and outs is None:
+            raise ValueError("accumulate needs existing outs")
+        descs = tensor_descs(tensors, outs, in_place=outs is None)
+    _here(descs.device, stream, norm, workspace)
+    with _made_on(stream):
+        ws = _workspace(lambda: tensors_workspace_bytes(descs), descs.device, workspace)
+    st = lib.dp_tensors_clip(descs.arr, len(descs.arr), _f32(norm, (1,), "norm"), float(C), int(bool(accumulate)),
+                             *_ws_args(ws), _stream_ptr(stream))
+    _check(st, "dp_tensors_clip")
+    return descs.outs
+
+
+def tensors_norm_clip(tensors, C: float, outs=None, *, accumulate: bool = False, norm: Optional[torch.Tensor] = None,
+                      tensor_norms: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                      descs: Optional[TensorDescs] = None, stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """tensors_norm, then tensors_clip with that norm, in one call (dp_tensors_norm_clip); in place without outs.
+    Returns the norm, float32 [1].  descs: the result of tensor_descs(tensors, outs)."""
+    lib = load_library()
+    if descs is None:
+        if accumulate and outs is None:
+            raise ValueError("accumulate needs existing outs")
+        descs = tensor_descs(tensors, outs, in_place=outs is None)
+    n = len(descs.arr)
+    _here(descs.device, stream, norm, tensor_norms, workspace)
+    with _made_on(stream):
+        if norm is None:
+            norm = torch.empty(1, dtype=torch.float32, device=descs.device)
+        ws = _workspace(lambda: tensors_workspace_bytes(descs), descs.device, workspace)
+    st = lib.dp_tensors_norm_clip(descs.arr, n, float(C), int(bool(accumulate)), _f32(norm, (1,), "norm"),
+                                  _f32(tensor_norms, (n,), "tensor_norms"), *_ws_args(ws), _stream_ptr(stream))
+    _check(st, "dp_tensors_norm_clip")
+    return norm
 
 
 def clipped_grad_rounds_inputs(B: int, T: int, d_in: int, d_out: int, dtype: int) -> bool:
