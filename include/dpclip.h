@@ -448,6 +448,50 @@ dp_status dp_tensors_norm_clip(const dp_tensor_desc* tensors, int64_t n_tensors,
 /* Scratch bytes for the three calls above; 0 for a number of tensors that they refuse. */
 size_t dp_tensors_workspace_bytes(int64_t n_tensors);
 
+/* A learned relative position bias of attention scores: a table with a number for
+ * each bucket of distances and each head, added to the scores before their softmax,
+ *     scores[b, h, q, k] += table[ bucket(k - q - q_start[b]), h ],
+ * and the gradient of that table for each example from the gradients dS of the
+ * scores (the sum over the positions that share a parameter, as in Eq.
+ * recurrent_gradient):
+ *     rows[b, j, h] = sum of dS[b, h, q, k] over the live (q, k) of bucket j.
+ * Query q of example b stands at position q + q_start[b], key k at position k.  A
+ * pair (q, k) is live if q < q_lens[b], k < k_lens[b] and, with `causal`, k <= q +
+ * q_start[b]; what is not live is neither read nor written, whatever is there. */
+typedef struct {
+    int64_t B, H, Tq, Tk;
+    int64_t s_b, s_h, s_q;     /* strides of the scores (or dS) in elements, >= 0; keys are next to each other */
+    int64_t o_b, o_h, o_q;     /* strides of dp_posbias_add's output */
+    const int32_t* buckets;    /* device, [2 reach + 1]: the bucket of each distance from -reach to reach; distances beyond
+                                  have the first or the last one's.  A bucket outside [0, n_buckets) adds nothing and gets
+                                  no gradient */
+    int64_t reach;             /* 0 to 2^20 */
+    int64_t n_buckets;         /* 1 to 1024 */
+    const int32_t* q_start;    /* NULL: 0 for all; or device int32[B] */
+    const int32_t* q_lens;     /* NULL: Tq for all; or device int32[B], taken as 0 below 0 and as Tq above Tq */
+    const int32_t* k_lens;     /* NULL: Tk for all; or device int32[B], likewise */
+    int causal;
+} dp_posbias_desc;
+
+/* out = scores + bias.  scores and out: device, `dtype` (DP_F32, DP_BF16 or DP_F16; 8-bit types give
+ * DP_ERR_UNSUPPORTED), aligned to one element; the sum is taken in float32 and rounded once.  out may be scores with
+ * the same strides; otherwise the memory from the first to the last element of either is apart, and no two elements of
+ * out share one.   table: device float32[n_buckets, H] */
+dp_status dp_posbias_add(const dp_posbias_desc* desc, const void* scores, const float* table, dp_dtype dtype,
+                         void* out, void* hip_stream);
+
+/* rows as above, and sqnorm[b] = (accumulate ? sqnorm[b] : 0) + ||rows[b]||^2.  The clipped sum of the rows is
+ * dp_clipped_bias_grad(rows, clip, B, n_buckets * H, ...).  The sums of the diagonals and buckets are taken in 64 bits.
+ *   dS         device, `dtype`, aligned to one element; the strides o_* are not looked at
+ *   rows       device float32[B, n_buckets, H], written
+ *   sqnorm     device float32[B]
+ *   workspace  device scratch of at least dp_posbias_workspace_bytes(B, H, Tq, Tk) bytes, 16-byte aligned */
+dp_status dp_posbias_sqnorm(const dp_posbias_desc* desc, const void* dS, dp_dtype dtype, int accumulate,
+                            float* sqnorm, float* rows, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Scratch bytes for dp_posbias_sqnorm; 0 for sizes that need none or that it refuses. */
+size_t dp_posbias_workspace_bytes(int64_t B, int64_t H, int64_t Tq, int64_t Tk);
+
 /* Gaussian mechanism (Section 2, Gaussian-mechanism lemma; Algorithm 1, the
  * update line): grad[j] += stddev * z[offset + j], j in [0, n), with z an
  * i.i.d. N(0,1) stream that is a pure function of (seed, element index):

@@ -90,6 +90,12 @@ struct ClippedBiasDesc { const float* u; const float* clip; int D; float* grad_b
 hipError_t launch_clipped_bias_layers(const ClippedBiasDesc* layers, int n_layers, int B, bool accumulate, float stddev, uint64_t seed, hipStream_t st);
 hipError_t launch_philox_raw(uint32_t* out, int64_t n_counters, uint64_t seed, uint64_t first, hipStream_t st);
 
+// ---- strided outputs (dp_api_posbias.hip): dimensions outside of `inner` elements next to each other
+struct StridedDim { int64_t size, stride; };
+int64_t span_elems(const StridedDim* dims, int n, int64_t inner);      // from the first to behind the last element; sizes of at least 1
+// whether no two elements share memory, each dimension outside of the ones of smaller strides; sorts dims
+bool elements_apart(StridedDim* dims, int n, int64_t inner);
+
 // ---- norm and clipping of a gradient of many tensors (dp_tensors.hip)
 struct TensorItem { const void* x; void* out; int64_t n; int first_chunk; short dt, odt; };      // types as above
 constexpr int kTensorChunk = 4096;     // elements of the smallest chunk
@@ -100,6 +106,21 @@ size_t tensors_ws_bytes(int64_t n_tensors);
 hipError_t launch_tensors_norm(const TensorItem* items, int n, int64_t chunk, int chunks, bool accumulate, float* norm, float* tensor_norms, void* ws, hipStream_t st);
 hipError_t launch_tensors_clip(const TensorItem* items, int n, int64_t chunk, int chunks, bool accumulate, const float* norm, float C, void* ws, hipStream_t st);
 hipError_t launch_tensors_norm_clip(const TensorItem* items, int n, int64_t chunk, int chunks, bool accumulate, float* norm, float* tensor_norms, float C, void* ws, hipStream_t st);
+
+// ---- relative position bias by buckets (dp_posbias.hip)
+struct PosbiasArgs {
+    int B, H, Tq, Tk;
+    int64_t s_b, s_h, s_q, o_b, o_h, o_q;
+    const int32_t* buckets; int reach, n_buckets;
+    const int32_t* q_start; const int32_t* q_lens; const int32_t* k_lens;
+    int causal;
+};
+constexpr int kMaxBuckets = 1024;
+bool posbias_fits(int64_t B, int64_t H, int64_t Tq, int64_t Tk);       // what the launches below hold
+size_t posbias_ws_bytes(int B, int H, int Tq, int Tk);
+hipError_t launch_posbias_add(const PosbiasArgs& a, const void* scores, const float* table, int dt, void* out, hipStream_t st);
+// rows [B, n_buckets, H]; their norms are launch_rows_sqnorm's
+hipError_t launch_posbias_rows(const PosbiasArgs& a, const void* dS, int dt, float* rows, void* ws, hipStream_t st);
 
 // ---- K-major ("TN") products  sum_k A[k,:]^T G[k,:]  (dp_tn_bf16.hip, dp_tn_f32.hip)
 struct TnPlan {

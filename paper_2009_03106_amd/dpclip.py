@@ -26,7 +26,8 @@ _PATHS = {"auto": DP_PATH_AUTO, "gram": DP_PATH_GRAM, "direct": DP_PATH_DIRECT}
 EXPORTS = ("dp_layer_sqnorm", "dp_layer_sqnorm_static", "dp_layers_sqnorm", "dp_layers_sqnorm_clip", "dp_layers_workspace_bytes", "dp_layers_clipped_grad",
            "dp_layers_clipped_grad_noise", "dp_layers_step", "dp_layers_clipped_workspace_bytes", "dp_clip_factors", "dp_clipped_grad", "dp_bias_sqnorm", "dp_clipped_bias_grad", "dp_layernorm_sqnorm",
            "dp_conv_sqnorm", "dp_conv_clipped_grad", "dp_conv_workspace_bytes", "dp_conv_rows_resident", "dp_add_noise", "dp_workspace_bytes", "dp_choose_path", "dp_status_string", "dp_philox_raw",
-           "dp_clipped_grad_rounds_inputs", "dp_tensors_norm", "dp_tensors_clip", "dp_tensors_norm_clip", "dp_tensors_workspace_bytes")
+           "dp_clipped_grad_rounds_inputs", "dp_tensors_norm", "dp_tensors_clip", "dp_tensors_norm_clip", "dp_tensors_workspace_bytes",
+           "dp_posbias_add", "dp_posbias_sqnorm", "dp_posbias_workspace_bytes")
 
 # the measurement probes and plan queries of include/dpclip_probes.h
 PROBE_EXPORTS = ("dp_probe_mfma", "dp_probe_read", "dp_probe_lds_read", "dp_plan_gram_wide", "dp_plan_sums_in_two_lengths")
@@ -47,6 +48,13 @@ class TensorDesc(ctypes.Structure):
     """dp_tensor_desc of the header."""
     _fields_ = [("x", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int),
                 ("out_dtype", ctypes.c_int)]
+
+
+class PosbiasDesc(ctypes.Structure):
+    """dp_posbias_desc of the header."""
+    _fields_ = ([(n, ctypes.c_int64) for n in ("B", "H", "Tq", "Tk", "s_b", "s_h", "s_q", "o_b", "o_h", "o_q")] +
+                [("buckets", ctypes.c_void_p), ("reach", ctypes.c_int64), ("n_buckets", ctypes.c_int64),
+                 ("q_start", ctypes.c_void_p), ("q_lens", ctypes.c_void_p), ("k_lens", ctypes.c_void_p), ("causal", ctypes.c_int)])
 
 
 class DpclipError(RuntimeError):
@@ -122,6 +130,12 @@ def load_library() -> ctypes.CDLL:
     lib.dp_tensors_norm_clip.restype = ci
     lib.dp_tensors_workspace_bytes.argtypes = [i64]
     lib.dp_tensors_workspace_bytes.restype = sz
+    lib.dp_posbias_add.argtypes = [ctypes.POINTER(PosbiasDesc), vp, vp, ci, vp, vp]
+    lib.dp_posbias_add.restype = ci
+    lib.dp_posbias_sqnorm.argtypes = [ctypes.POINTER(PosbiasDesc), vp, ci, ci, vp, vp, vp, sz, vp]
+    lib.dp_posbias_sqnorm.restype = ci
+    lib.dp_posbias_workspace_bytes.argtypes = [i64, i64, i64, i64]
+    lib.dp_posbias_workspace_bytes.restype = sz
     lib.dp_probe_mfma.argtypes = [ci, ci, i64, vp, ctypes.POINTER(ctypes.c_double), vp]
     lib.dp_probe_mfma.restype = ci
     lib.dp_probe_read.argtypes = [vp, sz, vp, vp]
@@ -741,6 +755,110 @@ def tensors_norm_clip(tensors, C: float, outs=None, *, accumulate: bool = False,
                                   _f32(tensor_norms, (n,), "tensor_norms"), *_ws_args(ws), _stream_ptr(stream))
     _check(st, "dp_tensors_norm_clip")
     return norm
+
+
+def relative_buckets(n_buckets: int, reach: int, both: bool = True, device="cuda") -> torch.Tensor:
+    """Buckets of the distances key minus query from -reach to reach, int32 [2 reach + 1]: half of the buckets hold a single
+    distance each, the others are ever wider up to reach, whose borders are equally far apart on a logarithmic scale.
+    both: the upper half of the buckets is for the keys behind the query; otherwise those share the bucket of distance 0.
+    Borders are compared in whole numbers, so no distance depends on a rounding."""
+    half = n_buckets // 2 if both else n_buckets
+    single = half // 2
+    wide = half - single
+    if n_buckets < 1 or reach < 0 or (both and n_buckets % 2) or half < 2 or reach <= single:
+        raise ValueError("needs at least two buckets on a side (an even number for both sides) and a reach beyond the single distances")
+    # border j of the wide ones: the smallest d with (d / single)^wide >= (reach / single)^j
+    back, j = [], 0
+    for d in range(reach + 1):
+        if d >= single:
+            while j + 1 < wide and d ** wide * single ** (j + 1) >= reach ** (j + 1) * single ** wide:
+                j += 1
+        back.append(d if d < single else single + j)
+    ahead = [half + b if both else 0 for b in back]
+    return torch.tensor(back[::-1] + ahead[1:], dtype=torch.int32, device=device)
+
+
+def _i32(t: Optional[torch.Tensor], n: int, name: str) -> Optional[int]:
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous int32 device tensor")
+    if t.numel() != n:
+        raise ValueError(f"{name} must hold {n} elements, got {tuple(t.shape)}")
+    return t.data_ptr() if n > 0 else None
+
+
+def _inner(t: torch.Tensor, dims: int, name: str) -> int:
+    """Address of a device tensor whose last dimension's elements are next to each other."""
+    if not t.is_cuda or t.dim() != dims or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name} must be a device tensor of {dims} dimensions, the last one's elements next to each other")
+    if _dtype_code(t) > DP_F16:
+        raise TypeError(f"unsupported dtype {t.dtype}")
+    return t.data_ptr() if t.numel() > 0 else 0
+
+
+def _posbias_desc(x: torch.Tensor, out: Optional[torch.Tensor], buckets, n_buckets: int, q_start, q_lens, k_lens, causal) -> PosbiasDesc:
+    B, H, Tq, Tk = x.shape
+    s = x.stride()
+    o = s if out is None else out.stride()
+    n = buckets.numel() if isinstance(buckets, torch.Tensor) else 0
+    if n % 2 == 0:
+        raise ValueError("buckets must hold one for each distance from -reach to reach")
+    return PosbiasDesc(B, H, Tq, Tk, s[0], s[1], s[2], o[0], o[1], o[2], _i32(buckets, n, "buckets"), n // 2, int(n_buckets),
+                       _i32(q_start, B, "q_start"), _i32(q_lens, B, "q_lens"), _i32(k_lens, B, "k_lens"), int(bool(causal)))
+
+
+def posbias_add(scores: torch.Tensor, table: torch.Tensor, buckets: torch.Tensor, out: Optional[torch.Tensor] = None, *,
+                q_start: Optional[torch.Tensor] = None, q_lens: Optional[torch.Tensor] = None,
+                k_lens: Optional[torch.Tensor] = None, causal: bool = False,
+                stream: Optional[torch.cuda.Stream] = None) -> torch.Tensor:
+    """out[b, h, q, k] = scores[b, h, q, k] + table[bucket of k - q - q_start[b], h] via dp_posbias_add, in place without
+    out.  scores and out: [B, H, Tq, Tk], any strides but for the keys'; table: float32 [n_buckets, H]; buckets: int32 of odd length,
+    one for each distance from -reach to reach (relative_buckets makes the usual ones); q_start, q_lens, k_lens: int32 [B].
+    Queries from q_lens[b] on, keys from k_lens[b] on and with causal the keys behind the query are left as they are in out."""
+    lib = load_library()
+    xp = _inner(scores, 4, "scores")
+    out = scores if out is None else out
+    op = _inner(out, 4, "out")
+    if out.shape != scores.shape or out.dtype != scores.dtype:
+        raise ValueError("out must have the shape and the dtype of scores")
+    if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.shape[1] != scores.shape[1]:
+        raise ValueError("table must be [n_buckets, H]")
+    _here(scores.device, stream, out, table, buckets, q_start, q_lens, k_lens)
+    d = _posbias_desc(scores, out, buckets, table.shape[0], q_start, q_lens, k_lens, causal)
+    st = lib.dp_posbias_add(ctypes.byref(d), xp, _f32(table, table.shape, "table"), _dtype_code(scores), op, _stream_ptr(stream))
+    _check(st, "dp_posbias_add")
+    return out
+
+
+def posbias_workspace_bytes(dS: torch.Tensor) -> int:
+    return int(load_library().dp_posbias_workspace_bytes(*dS.shape))
+
+
+def posbias_sqnorm(dS: torch.Tensor, buckets: torch.Tensor, n_buckets: int, sqnorm: Optional[torch.Tensor] = None,
+                   rows: Optional[torch.Tensor] = None, *, accumulate: bool = False, q_start: Optional[torch.Tensor] = None,
+                   q_lens: Optional[torch.Tensor] = None, k_lens: Optional[torch.Tensor] = None, causal: bool = False,
+                   workspace: Optional[torch.Tensor] = None, stream: Optional[torch.cuda.Stream] = None):
+    """rows[b, j, h] = sum of dS[b, h, q, k] over bucket j, the per-example gradients of posbias_add's table, and sqnorm[b]
+    (+)= ||rows[b]||^2 via dp_posbias_sqnorm; the arguments are posbias_add's.  Returns (sqnorm, rows); the clipped sum is
+    clipped_bias_grad(rows.view(B, -1), clip)."""
+    lib = load_library()
+    xp = _inner(dS, 4, "dS")
+    B, H = dS.shape[0], dS.shape[1]
+    if sqnorm is None and accumulate:
+        raise ValueError("accumulate needs an existing sqnorm tensor")
+    _here(dS.device, stream, sqnorm, rows, buckets, q_start, q_lens, k_lens, workspace)
+    d = _posbias_desc(dS, None, buckets, n_buckets, q_start, q_lens, k_lens, causal)
+    with _made_on(stream):
+        if sqnorm is None:
+            sqnorm = torch.empty(B, dtype=torch.float32, device=dS.device)
+        if rows is None:
+            rows = torch.empty((B, n_buckets, H), dtype=torch.float32, device=dS.device)
+        ws = _workspace(lambda: posbias_workspace_bytes(dS), dS.device, workspace)
+    st = lib.dp_posbias_sqnorm(ctypes.byref(d), xp, _dtype_code(dS), int(bool(accumulate)), _f32(sqnorm, (B,), "sqnorm"),
+                               _f32(rows, (B, n_buckets, H), "rows"), *_ws_args(ws), _stream_ptr(stream))
+    _check(st, "dp_posbias_sqnorm")
+    return sqnorm, rows
 
 
 def clipped_grad_rounds_inputs(B: int, T: int, d_in: int, d_out: int, dtype: int) -> bool:
