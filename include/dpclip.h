@@ -475,8 +475,7 @@ typedef struct {
 
 /* out = scores + bias.  scores and out: device, `dtype` (DP_F32, DP_BF16 or DP_F16; 8-bit types give
  * DP_ERR_UNSUPPORTED), aligned to one element; the sum is taken in float32 and rounded once.  out may be scores with
- * the same strides; otherwise the memory from the first to the last element of either is apart, and no two elements of
- * out share one.   table: device float32[n_buckets, H] */
+ * the same strides; otherwise no element of out is one of scores, and no two elements of out share one.   table: device float32[n_buckets, H] */
 dp_status dp_posbias_add(const dp_posbias_desc* desc, const void* scores, const float* table, dp_dtype dtype,
                          void* out, void* hip_stream);
 
@@ -491,6 +490,58 @@ dp_status dp_posbias_sqnorm(const dp_posbias_desc* desc, const void* dS, dp_dtyp
 
 /* Scratch bytes for dp_posbias_sqnorm; 0 for sizes that need none or that it refuses. */
 size_t dp_posbias_workspace_bytes(int64_t B, int64_t H, int64_t Tq, int64_t Tk);
+
+/* Norms of queries and keys for each head, with the position rotation in the same
+ * pass.  For a row x (a head of a token, D numbers) with gain w:
+ *     r = 1 / sqrt(mean(x^2) + eps),   y = R(p) (x r (*) w),
+ * R(p) turns the pairs of the first `rot` numbers by the angles p freqs[j], p the token's
+ * position; the numbers behind them stay.  Pairs are (j, j + rot / 2) or neighbours
+ * (2 j, 2 j + 1).  Angles are taken in 64 bits, everything else in float32, y is
+ * rounded once.  dp_headnorm_sqnorm is the backward pass: with u = R(p)^T dy,
+ *     dx              = r (u (*) w - x r mean(u (*) w (*) x r)),
+ *     gain_rows[i, :] = sum over example i's tokens and heads of u (*) x r,
+ * the per-example gradient of the gain (the sum over the positions and heads that
+ * share it, as in Algorithm 5), and its squared norm. */
+typedef enum { DP_ROTATE_HALVES = 0, DP_ROTATE_PAIRS = 1 } dp_rotation;
+
+typedef struct {
+    const void* x;             /* device, `dtype`, aligned to one element: [B, T, H, D] with the strides below (in elements,
+                                  >= 0), the D numbers of a row next to each other; read only unless out is x */
+    int64_t x_b, x_t, x_h;
+    int64_t H;                 /* heads (queries and keys may have different numbers) */
+    const float* gain;         /* device float32[D] */
+    void* out;                 /* device, `dtype`: y, or dx.  May be x (or dy) itself with the same strides; no other element of
+                                  any out of the call is an element of an input or of another out */
+    int64_t o_b, o_t, o_h;
+    const void* dy;            /* dp_headnorm_sqnorm only: the gradient of y */
+    int64_t dy_b, dy_t, dy_h;
+    float* gain_rows;          /* dp_headnorm_sqnorm only: device float32[B, D], written */
+} dp_heads_desc;
+
+typedef struct {
+    int64_t B, T, D;           /* D at most 1024 */
+    int64_t rot;               /* even, 0 to D */
+    dp_rotation rotation;
+    float eps;                 /* > 0 */
+    const int32_t* positions;  /* NULL: token t has position t; or device int32, token t of example b at b * positions_b + t */
+    int64_t positions_b;       /* >= 0; 0: all examples share one row */
+    const double* freqs;       /* device, [rot / 2], angle per position in radians; may be NULL if rot is 0 */
+    const int32_t* lengths;    /* NULL, or device int32[B]: tokens from lengths[b] on are neither read nor written and count
+                                  for nothing (taken as 0 below 0 and as T above T) */
+} dp_headnorm_desc;
+
+/*   heads, n_heads  HOST array of 1 or 2 descriptors: queries, and keys
+ *   dtype           DP_F32, DP_BF16 or DP_F16 (8-bit types give DP_ERR_UNSUPPORTED) */
+dp_status dp_headnorm(const dp_headnorm_desc* desc, const dp_heads_desc* heads, int64_t n_heads, dp_dtype dtype, void* hip_stream);
+
+/*     sqnorm[i] = (accumulate ? sqnorm[i] : 0) + sum over the descriptors of ||gain_rows[i]||^2
+ * The clipped sum of the rows is dp_clipped_bias_grad(gain_rows, clip, B, D, ...).
+ *   workspace  device scratch of at least dp_headnorm_workspace_bytes(n_heads, B, T, D) bytes, 16-byte aligned */
+dp_status dp_headnorm_sqnorm(const dp_headnorm_desc* desc, const dp_heads_desc* heads, int64_t n_heads, dp_dtype dtype,
+                             int accumulate, float* sqnorm, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Scratch bytes for dp_headnorm_sqnorm; 0 for sizes that need none or that it refuses. */
+size_t dp_headnorm_workspace_bytes(int64_t n_heads, int64_t B, int64_t T, int64_t D);
 
 /* Gaussian mechanism (Section 2, Gaussian-mechanism lemma; Algorithm 1, the
  * update line): grad[j] += stddev * z[offset + j], j in [0, n), with z an

@@ -1,18 +1,14 @@
 // C-ABI entry points of the relative position bias (include/dpclip.h): argument checks and launches.
 #include "../../include/dpclip.h"
 #include "dp_internal.h"
-#include <algorithm>
 
 using namespace dpk;
 
 namespace {
 
 constexpr int64_t kMaxReach = int64_t(1) << 20;
-constexpr int64_t kMaxOffset = int64_t(1) << 48;       // of an element along one dimension: no address passes 64 bits
 
 bool element_aligned(const void* p, dp_dtype d) { return reinterpret_cast<uintptr_t>(p) % (d == DP_F32 ? 4 : 2) == 0; }
-
-bool too_far(int64_t size, int64_t stride) { return size > 1 && stride > kMaxOffset / (size - 1); }
 
 dp_status check(const dp_posbias_desc* d, dp_dtype dtype) {
     if (!d || d->B < 0 || d->H < 0 || d->Tq < 0 || d->Tk < 0 || d->reach < 0 || d->n_buckets < 1) return DP_ERR_INVALID_ARG;
@@ -32,27 +28,6 @@ PosbiasArgs args_of(const dp_posbias_desc& d) {
 
 }  // namespace
 
-namespace dpk {
-
-int64_t span_elems(const StridedDim* dims, int n, int64_t inner) {
-    int64_t last = inner;
-    for (int i = 0; i < n; ++i) last += (dims[i].size - 1) * dims[i].stride;
-    return last;
-}
-
-bool elements_apart(StridedDim* dims, int n, int64_t inner) {
-    std::sort(dims, dims + n, [](const StridedDim& a, const StridedDim& b) { return a.stride < b.stride; });
-    int64_t extent = inner;
-    for (int i = 0; i < n; ++i) {
-        if (dims[i].size <= 1) continue;
-        if (dims[i].stride < extent) return false;
-        extent += (dims[i].size - 1) * dims[i].stride;
-    }
-    return true;
-}
-
-}  // namespace dpk
-
 extern "C" {
 
 size_t dp_posbias_workspace_bytes(int64_t B, int64_t H, int64_t Tq, int64_t Tk) {
@@ -68,12 +43,9 @@ dp_status dp_posbias_add(const dp_posbias_desc* desc, const void* scores, const 
     if (too_far(d.B, d.o_b) || too_far(d.H, d.o_h) || too_far(d.Tq, d.o_q)) return DP_ERR_UNSUPPORTED;
     if (empty(d)) return DP_OK;
     if (!scores || !table || !out || !d.buckets || !element_aligned(scores, dtype) || !element_aligned(out, dtype)) return DP_ERR_INVALID_ARG;
-    StridedDim in[3] = {{d.B, d.s_b}, {d.H, d.s_h}, {d.Tq, d.s_q}}, to[3] = {{d.B, d.o_b}, {d.H, d.o_h}, {d.Tq, d.o_q}};
-    const size_t es = dtype == DP_F32 ? 4 : 2;
-    const uintptr_t x = (uintptr_t)scores, o = (uintptr_t)out;
-    const bool same = x == o && d.s_b == d.o_b && d.s_h == d.o_h && d.s_q == d.o_q;
-    if (!same && x < o + es * span_elems(to, 3, d.Tk) && o < x + es * span_elems(in, 3, d.Tk)) return DP_ERR_INVALID_ARG;
-    if (!elements_apart(to, 3, d.Tk)) return DP_ERR_INVALID_ARG;
+    const int es = dtype == DP_F32 ? 4 : 2;
+    const Strided in{scores, {d.B, d.H, d.Tq}, {d.s_b, d.s_h, d.s_q}, d.Tk, es}, to{out, {d.B, d.H, d.Tq}, {d.o_b, d.o_h, d.o_q}, d.Tk, es};
+    if (!elements_apart(to) || !(same_layout(in, to) || tensors_apart(in, to))) return DP_ERR_INVALID_ARG;
     const hipError_t e = launch_posbias_add(args_of(d), scores, table, (int)dtype, out, static_cast<hipStream_t>(hip_stream));
     return e == hipSuccess ? DP_OK : DP_ERR_HIP;
 }

@@ -1,0 +1,335 @@
+// Norms of queries and keys for each head with the position rotation in the same pass, and their backward pass with the
+// per-example gradients of the gains:
+//     r = 1 / sqrt(mean(x^2) + eps),  y = R(p) (x r (*) w)
+//     u = R(p)^T dy,  dx = r (u (*) w - x r mean(u (*) w (*) x r)),  gain_rows[i] = sum_{t, h} u (*) x r
+// Bound by memory: a row is read once into registers (two rows in the backward pass) and one is written.
+//
+// A row of D numbers is the registers of L lanes of a wave, as pairs that turn together; the 64 / L rows of a wave are `hw`
+// heads of `tw` tokens, hw tw = 64 / L.  The sines and cosines of a token's angles serve all of its heads.
+#include <algorithm>
+#include "dp_elems.h"
+#include "dp_internal.h"
+
+namespace dpk {
+
+namespace {
+
+// What a launch works on: how rows are dealt to lanes.
+struct Rows {
+    int L, hw, tw;             // lanes of a row, heads and tokens of a wave at a time (powers of two)
+    int its0, its;             // steps over the heads: of the first descriptor, of both
+    int split;                 // waves that share a token's steps
+};
+
+// The pairs of a row: V next to each other at a time, N times for a lane.
+//   V == 1: pair p of lane l is l + i L; its numbers are columns a and b (b beyond D: none)
+//   V == 8: pair 8 l and the seven behind; D and rot are multiples of 16
+// PAIRS (V == 8): neighbours turn together, so the 16 columns are one piece.
+__device__ __forceinline__ int2 columns(const HeadnormArgs& a, int p) {
+    if (a.pairs) return make_int2(2 * p, 2 * p + 1);
+    const int half = a.rot / 2;
+    return p < half ? make_int2(p, p + half) : make_int2(2 * p, 2 * p + 1);
+}
+
+template <int DT, int V, int N, bool PAIRS> struct Row {
+    float lo[V * N], hi[V * N];            // the pairs' numbers: (lo[i], hi[i]) turn together (PAIRS: neighbours within lo and within hi)
+
+    __device__ __forceinline__ void load(const HeadnormArgs& a, const void* p, int64_t at, int l, int L, bool live) {
+        static_assert(V == 1, "one pair at a time");
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int2 c = columns(a, l + i * L);
+            lo[i] = live && c.x < a.D ? load_one<DT>(p, at + c.x) : 0.f;
+            hi[i] = live && c.y < a.D ? load_one<DT>(p, at + c.y) : 0.f;
+        }
+    }
+    __device__ __forceinline__ void store(const HeadnormArgs& a, void* p, int64_t at, int l, int L) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int2 c = columns(a, l + i * L);
+            if (c.x < a.D) store_one<DT>(p, at + c.x, lo[i]);
+            if (c.y < a.D) store_one<DT>(p, at + c.y, hi[i]);
+        }
+    }
+    __device__ __forceinline__ void to_lds(const HeadnormArgs& a, float* row, int l, int L) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int2 c = columns(a, l + i * L);
+            if (c.x < a.D) row[c.x] = lo[i];
+            if (c.y < a.D) row[c.y] = hi[i];
+        }
+    }
+};
+
+// sine and cosine of position * freq.  The angle is taken in turns and in 64 bits: what is left of it after the whole quarters is
+// at most an eighth of a turn, exact to 2^-53 of the position's turns, and the series below are exact to float32 there (the first
+// terms left out: x^11 / 11! < 2e-9, x^12 / 12! < 2e-10 for x up to pi / 4).
+__device__ __forceinline__ void sincos_of(int position, double freq, float& s, float& c) {
+    const double turns = (double)position * (freq * 0.15915494309189533577);
+    const double quarters = rint(turns * 4.0);
+    const float x = (float)((turns - quarters * 0.25) * 6.283185307179586477);
+    const int q = (int)(int64_t)(quarters - 4.0 * floor(quarters * 0.25));          // 0 to 3
+    const float z = x * x;
+    const float sx = x + x * z * (-1.6666667e-1f + z * (8.3333333e-3f + z * (-1.9841270e-4f + z * 2.7557319e-6f)));
+    const float cx = 1.0f + z * (-0.5f + z * (4.1666667e-2f + z * (-1.3888889e-3f + z * (2.4801587e-5f + z * -2.7557319e-7f))));
+    s = q & 1 ? cx : sx;
+    c = q & 1 ? sx : cx;
+    if (q & 2) s = -s;
+    if (q == 1 || q == 2) c = -c;
+}
+
+// the turn of each pair of a lane; pairs behind the rotated ones do not turn
+template <int V, int N> struct Turn {
+    float s[V * N], c[V * N];
+    __device__ __forceinline__ void of(const HeadnormArgs& a, int position, int l, int L, bool live) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int p = (l + i * L) * V + v, k = i * V + v;
+                s[k] = 0.f;
+                c[k] = 1.f;
+                if (live && p < a.rot / 2) sincos_of(position, a.freqs[p], s[k], c[k]);
+            }
+    }
+};
+
+__device__ __forceinline__ float row_sum(float v, int L) {
+    for (int off = L >> 1; off > 0; off >>= 1) v += __shfl_xor(v, off, kWave);
+    return v;
+}
+
+struct Token { int b, t, position; bool live; };
+__device__ __forceinline__ Token token_of(const HeadnormArgs& a, int64_t n) {
+    Token k;
+    k.live = n < (int64_t)a.B * a.T;
+    const int64_t at = k.live ? n : 0;
+    k.b = (int)(at / a.T);
+    k.t = (int)(at - (int64_t)k.b * a.T);
+    if (a.lengths) k.live = k.live && k.t < a.lengths[k.b];
+    k.position = a.positions ? a.positions[k.b * a.positions_b + k.t] : k.t;
+    return k;
+}
+
+// A wave takes tw tokens at a time and its share of the steps over their heads.
+template <int DT, int V, int N, bool PAIRS>
+__global__ __launch_bounds__(kThreads) void k_headnorm(HeadnormArgs a, Rows w) {
+    const int lane = threadIdx.x & (kWave - 1), l = lane & (w.L - 1), g = lane / w.L;
+    const int64_t wave = (int64_t)blockIdx.x * (kThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t step = (int64_t)gridDim.x * (kThreads / kWave) / w.split;
+    const int part = (int)(wave % w.split);
+    const int it0 = (int)((int64_t)w.its * part / w.split), it1 = (int)((int64_t)w.its * (part + 1) / w.split);
+    const float mean = 1.0f / a.D;
+    for (int64_t n0 = wave / w.split * w.tw; n0 < (int64_t)a.B * a.T; n0 += step * w.tw) {
+        const Token k = token_of(a, n0 + g / w.hw);
+        Turn<V, N> turn;
+        turn.of(a, k.position, l, w.L, k.live);
+        for (int it = it0; it < it1; ++it) {
+            const int which = it >= w.its0;
+            const HeadsArgs& hd = a.heads[which];
+            const int h = (which ? it - w.its0 : it) * w.hw + (g & (w.hw - 1));
+            const bool live = k.live && h < hd.H;
+            Row<DT, V, N, PAIRS> x;
+            Row<0, V, N, PAIRS> gain;
+            x.load(a, hd.x, k.b * hd.x_b + k.t * hd.x_t + h * hd.x_h, l, w.L, live);
+            gain.load(a, hd.gain, 0, l, w.L, true);
+            float sq = 0.f;
+#pragma unroll
+            for (int i = 0; i < V * N; ++i) sq += x.lo[i] * x.lo[i] + x.hi[i] * x.hi[i];
+            const float r = 1.0f / sqrtf(row_sum(sq, w.L) * mean + a.eps);
+#pragma unroll
+            for (int i = 0; i < V * N; ++i) {
+                const float lo = x.lo[i] * r * gain.lo[i], hi = x.hi[i] * r * gain.hi[i];
+                x.lo[i] = lo * turn.c[i] - hi * turn.s[i];
+                x.hi[i] = lo * turn.s[i] + hi * turn.c[i];
+            }
+            if (live) x.store(a, hd.out, k.b * hd.o_b + k.t * hd.o_t + h * hd.o_h, l, w.L);
+        }
+    }
+}
+
+// Backward.  A workgroup has `tokens` of an example's tokens; its sums of the gains' gradients go to partial[b][chunk][descriptor][D].
+template <int DT, int V, int N, bool PAIRS>
+__global__ __launch_bounds__(kThreads) void k_headnorm_back(HeadnormArgs a, Rows w, int tokens, int chunks, float* __restrict__ partial) {
+    extern __shared__ float sums[];                    // [waves][descriptors][D]
+    constexpr int kWaves = kThreads / kWave;
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane & (w.L - 1), g = lane / w.L;
+    const int b = blockIdx.x / chunks, chunk = blockIdx.x - b * chunks;
+    const int t0 = chunk * tokens, t1 = min(t0 + tokens, a.T);
+    const float mean = 1.0f / a.D;
+    Row<0, V, N, PAIRS> acc[2] = {};
+    for (int base = t0 + wave * w.tw; base < t1; base += kWaves * w.tw) {
+        const int t = base + g / w.hw;
+        Token k = token_of(a, (int64_t)b * a.T + min(t, t1 - 1));
+        k.live = k.live && t < t1;
+        Turn<V, N> turn;
+        turn.of(a, k.position, l, w.L, k.live);
+        auto step = [&](const HeadsArgs& hd, int it, Row<0, V, N, PAIRS>& gg) {
+            const int h = it * w.hw + (g & (w.hw - 1));
+            const bool live = k.live && h < hd.H;
+            Row<DT, V, N, PAIRS> x, u;
+            Row<0, V, N, PAIRS> gain;
+            x.load(a, hd.x, k.b * hd.x_b + k.t * hd.x_t + h * hd.x_h, l, w.L, live);
+            u.load(a, hd.dy, k.b * hd.dy_b + k.t * hd.dy_t + h * hd.dy_h, l, w.L, live);
+            gain.load(a, hd.gain, 0, l, w.L, true);
+            float sq = 0.f;
+#pragma unroll
+            for (int i = 0; i < V * N; ++i) sq += x.lo[i] * x.lo[i] + x.hi[i] * x.hi[i];
+            const float r = 1.0f / sqrtf(row_sum(sq, w.L) * mean + a.eps);
+            float dot = 0.f;
+#pragma unroll
+            for (int i = 0; i < V * N; ++i) {
+                const float lo = u.lo[i] * turn.c[i] + u.hi[i] * turn.s[i], hi = u.hi[i] * turn.c[i] - u.lo[i] * turn.s[i];
+                x.lo[i] *= r;
+                x.hi[i] *= r;
+                gg.lo[i] += lo * x.lo[i];
+                gg.hi[i] += hi * x.hi[i];
+                u.lo[i] = lo * gain.lo[i];
+                u.hi[i] = hi * gain.hi[i];
+                dot += u.lo[i] * x.lo[i] + u.hi[i] * x.hi[i];
+            }
+            dot = row_sum(dot, w.L) * mean;
+#pragma unroll
+            for (int i = 0; i < V * N; ++i) {
+                x.lo[i] = r * (u.lo[i] - x.lo[i] * dot);
+                x.hi[i] = r * (u.hi[i] - x.hi[i] * dot);
+            }
+            if (live) x.store(a, hd.out, k.b * hd.o_b + k.t * hd.o_t + h * hd.o_h, l, w.L);
+        };
+        for (int it = 0; it < w.its0; ++it) step(a.heads[0], it, acc[0]);
+        for (int it = w.its0; it < w.its; ++it) step(a.heads[1], it - w.its0, acc[1]);
+    }
+    // the rows of a wave, then the waves, in a fixed order
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        if (which >= a.n_heads) break;
+#pragma unroll
+        for (int i = 0; i < V * N; ++i)
+            for (int off = w.L; off < kWave; off <<= 1) {
+                acc[which].lo[i] += __shfl_xor(acc[which].lo[i], off, kWave);
+                acc[which].hi[i] += __shfl_xor(acc[which].hi[i], off, kWave);
+            }
+        if (g == 0) acc[which].to_lds(a, sums + (wave * a.n_heads + which) * a.D, l, w.L);
+    }
+    __syncthreads();
+    const int n = a.n_heads * a.D;
+    for (int j = threadIdx.x; j < n; j += kThreads)
+        partial[(int64_t)blockIdx.x * n + j] = (sums[j] + sums[n + j]) + (sums[2 * n + j] + sums[3 * n + j]);
+}
+
+// A workgroup per example: the chunks' sums, and the squared norm of the rows.
+__global__ __launch_bounds__(kThreads) void k_headnorm_fold(HeadnormArgs a, int chunks, const float* __restrict__ partial, int accumulate, float* __restrict__ sqnorm) {
+    __shared__ double red[4];
+    const int b = blockIdx.x, n = a.n_heads * a.D;
+    const float* p = partial + (int64_t)b * chunks * n;
+    double sq = 0.0;
+    for (int j = threadIdx.x; j < n; j += kThreads) {
+        double s = 0.0;
+        for (int c = 0; c < chunks; ++c) s += p[(int64_t)c * n + j];
+        const float v = (float)s;
+        const int which = j >= a.D;
+        a.heads[which].gain_rows[(int64_t)b * a.D + (which ? j - a.D : j)] = v;
+        sq += (double)v * v;
+    }
+    sq = block_sum_256_f64(sq, red);
+    if (threadIdx.x == 0) sqnorm[b] = (float)(accumulate ? sqnorm[b] + sq : sq);
+}
+
+int pow2_up(int n) {
+    int p = 1;
+    while (p < n) p *= 2;
+    return p;
+}
+
+// pairs of a lane and lanes of a row
+struct Shape { int V, N, L; };
+Shape shape_of(const HeadnormArgs& a) {
+    const int pairs = (a.D + 1) / 2, L = std::min(kWave, pow2_up(pairs));
+    return Shape{1, pow2_up((pairs + L - 1) / L), L};
+}
+
+// Heads and tokens of a wave: as many heads (which lie next to each other) as leave at most a tenth of the rows idle, else the
+// number with the fewest idle ones.
+Rows rows_of(const HeadnormArgs& a, int L) {
+    const int W = kWave / L, H0 = a.heads[0].H, H1 = a.heads[1].H;
+    Rows w{};
+    w.L = L;
+    int64_t least = INT64_MAX;
+    for (int hw = W; hw >= 1; hw /= 2) {
+        const int i0 = ceil_div(H0, hw), i1 = ceil_div(H1, hw);
+        const int64_t taken = (int64_t)hw * (i0 + i1);
+        if (taken >= least) continue;
+        least = taken;
+        w.hw = hw; w.tw = W / hw; w.its0 = i0; w.its = i0 + i1;
+        if (taken * 10 <= (int64_t)(H0 + H1) * 11) break;
+    }
+    w.split = 1;
+    return w;
+}
+
+// Chunks of an example's tokens in the backward pass: about eight workgroups for each of the 256 compute units, of at least 16 tokens.
+int back_chunks(int B, int T) {
+    return (int)std::max<int64_t>(1, std::min<int64_t>({512, (2048 + B - 1) / (int64_t)B, (T + 15) / 16}));
+}
+
+template <int DT, int V, int N, bool PAIRS> void forward_as(const HeadnormArgs& a, const Rows& w, int grid, hipStream_t st) {
+    k_headnorm<DT, V, N, PAIRS><<<grid, kThreads, 0, st>>>(a, w);
+}
+template <int DT, int V, int N, bool PAIRS> void backward_as(const HeadnormArgs& a, const Rows& w, int tokens, int chunks, float* partial, hipStream_t st) {
+    const size_t lds = (size_t)(kThreads / kWave) * a.n_heads * a.D * sizeof(float);
+    k_headnorm_back<DT, V, N, PAIRS><<<a.B * chunks, kThreads, lds, st>>>(a, w, tokens, chunks, partial);
+}
+
+template <int DT> void forward(const HeadnormArgs& a, const Shape& s, const Rows& w, int grid, hipStream_t st) {
+    if (s.N == 1)      forward_as<DT, 1, 1, false>(a, w, grid, st);
+    else if (s.N == 2) forward_as<DT, 1, 2, false>(a, w, grid, st);
+    else if (s.N == 4) forward_as<DT, 1, 4, false>(a, w, grid, st);
+    else               forward_as<DT, 1, 8, false>(a, w, grid, st);
+}
+template <int DT> void backward(const HeadnormArgs& a, const Shape& s, const Rows& w, int tokens, int chunks, float* partial, hipStream_t st) {
+    if (s.N == 1)      backward_as<DT, 1, 1, false>(a, w, tokens, chunks, partial, st);
+    else if (s.N == 2) backward_as<DT, 1, 2, false>(a, w, tokens, chunks, partial, st);
+    else if (s.N == 4) backward_as<DT, 1, 4, false>(a, w, tokens, chunks, partial, st);
+    else               backward_as<DT, 1, 8, false>(a, w, tokens, chunks, partial, st);
+}
+
+}  // namespace
+
+bool headnorm_fits(int64_t B, int64_t T, int64_t H0, int64_t H1) {
+    const int64_t most = int64_t(1) << 30;
+    if (B > (int64_t(1) << 22) || T > most || H0 > most || H1 > most) return false;
+    return B == 0 || T <= most / B;
+}
+size_t headnorm_ws_bytes(int n_heads, int B, int T, int D) { return (size_t)B * back_chunks(B, T) * n_heads * D * sizeof(float); }
+
+hipError_t launch_headnorm(const HeadnormArgs& a, int dt, hipStream_t st) {
+    const Shape s = shape_of(a);
+    Rows w = rows_of(a, s.L);
+    // a wave for every tw tokens; where that leaves the chip empty, several waves share a token's heads
+    const int64_t groups = ((int64_t)a.B * a.T + w.tw - 1) / w.tw;
+    w.split = (int)std::max<int64_t>(1, std::min<int64_t>(w.its, 4096 / groups));
+    const int64_t wgs = (groups * w.split + kThreads / kWave - 1) / (kThreads / kWave);
+    int grid = (int)std::min<int64_t>(wgs, 1 << 14);
+    // whole tokens: a multiple of split waves
+    while ((int64_t)grid * (kThreads / kWave) % w.split) ++grid;
+    if (dt == 0)      forward<0>(a, s, w, grid, st);
+    else if (dt == 1) forward<1>(a, s, w, grid, st);
+    else              forward<2>(a, s, w, grid, st);
+    return hipGetLastError();
+}
+
+hipError_t launch_headnorm_sqnorm(const HeadnormArgs& a, int dt, bool accumulate, float* sqnorm, void* ws, hipStream_t st) {
+    const Shape s = shape_of(a);
+    const Rows w = rows_of(a, s.L);
+    const int chunks = back_chunks(a.B, a.T), tokens = ceil_div(a.T, chunks);
+    float* partial = static_cast<float*>(ws);
+    if (dt == 0)      backward<0>(a, s, w, tokens, chunks, partial, st);
+    else if (dt == 1) backward<1>(a, s, w, tokens, chunks, partial, st);
+    else              backward<2>(a, s, w, tokens, chunks, partial, st);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    k_headnorm_fold<<<a.B, kThreads, 0, st>>>(a, chunks, partial, accumulate, sqnorm);
+    return hipGetLastError();
+}
+
+}  // namespace dpk

@@ -90,11 +90,17 @@ struct ClippedBiasDesc { const float* u; const float* clip; int D; float* grad_b
 hipError_t launch_clipped_bias_layers(const ClippedBiasDesc* layers, int n_layers, int B, bool accumulate, float stddev, uint64_t seed, hipStream_t st);
 hipError_t launch_philox_raw(uint32_t* out, int64_t n_counters, uint64_t seed, uint64_t first, hipStream_t st);
 
-// ---- strided outputs (dp_api_posbias.hip): dimensions outside of `inner` elements next to each other
-struct StridedDim { int64_t size, stride; };
-int64_t span_elems(const StridedDim* dims, int n, int64_t inner);      // from the first to behind the last element; sizes of at least 1
-// whether no two elements share memory, each dimension outside of the ones of smaller strides; sorts dims
-bool elements_apart(StridedDim* dims, int n, int64_t inner);
+// ---- strided tensors (dp_api_strided.hip): three dimensions (sizes of at least 1, strides >= 0) outside of `inner` elements next
+// to each other, all in elements of `es` bytes
+struct Strided { const void* p; int64_t size[3], stride[3], inner; int es; };
+// whether an element's offset may pass 2^48 elements along a dimension: no address passes 64 bits below
+bool too_far(int64_t size, int64_t stride);
+// whether no two elements share memory, with each dimension outside of the ones of smaller strides
+bool elements_apart(const Strided& a);
+// whether no element of one lies in the other: their spans are apart, or they advance together along their outermost dimension
+// and are apart within one step of it
+bool tensors_apart(const Strided& a, const Strided& b);
+bool same_layout(const Strided& a, const Strided& b);
 
 // ---- norm and clipping of a gradient of many tensors (dp_tensors.hip)
 struct TensorItem { const void* x; void* out; int64_t n; int first_chunk; short dt, odt; };      // types as above
@@ -121,6 +127,22 @@ size_t posbias_ws_bytes(int B, int H, int Tq, int Tk);
 hipError_t launch_posbias_add(const PosbiasArgs& a, const void* scores, const float* table, int dt, void* out, hipStream_t st);
 // rows [B, n_buckets, H]; their norms are launch_rows_sqnorm's
 hipError_t launch_posbias_rows(const PosbiasArgs& a, const void* dS, int dt, float* rows, void* ws, hipStream_t st);
+
+// ---- norms of queries and keys with the rotation (dp_headnorm.hip)
+struct HeadsArgs { const void* x; int64_t x_b, x_t, x_h; int H; const float* gain; void* out; int64_t o_b, o_t, o_h; const void* dy; int64_t dy_b, dy_t, dy_h; float* gain_rows; };
+struct HeadnormArgs {
+    HeadsArgs heads[2]; int n_heads;
+    int B, T, D, rot, pairs;
+    float eps;
+    const int32_t* positions; int64_t positions_b;
+    const double* freqs;
+    const int32_t* lengths;
+};
+constexpr int kMaxHeadDim = 1024;
+bool headnorm_fits(int64_t B, int64_t T, int64_t H0, int64_t H1);
+size_t headnorm_ws_bytes(int n_heads, int B, int T, int D);
+hipError_t launch_headnorm(const HeadnormArgs& a, int dt, hipStream_t st);
+hipError_t launch_headnorm_sqnorm(const HeadnormArgs& a, int dt, bool accumulate, float* sqnorm, void* ws, hipStream_t st);
 
 // ---- K-major ("TN") products  sum_k A[k,:]^T G[k,:]  (dp_tn_bf16.hip, dp_tn_f32.hip)
 struct TnPlan {

@@ -27,7 +27,8 @@ EXPORTS = ("dp_layer_sqnorm", "dp_layer_sqnorm_static", "dp_layers_sqnorm", "dp_
            "dp_layers_clipped_grad_noise", "dp_layers_step", "dp_layers_clipped_workspace_bytes", "dp_clip_factors", "dp_clipped_grad", "dp_bias_sqnorm", "dp_clipped_bias_grad", "dp_layernorm_sqnorm",
            "dp_conv_sqnorm", "dp_conv_clipped_grad", "dp_conv_workspace_bytes", "dp_conv_rows_resident", "dp_add_noise", "dp_workspace_bytes", "dp_choose_path", "dp_status_string", "dp_philox_raw",
            "dp_clipped_grad_rounds_inputs", "dp_tensors_norm", "dp_tensors_clip", "dp_tensors_norm_clip", "dp_tensors_workspace_bytes",
-           "dp_posbias_add", "dp_posbias_sqnorm", "dp_posbias_workspace_bytes")
+           "dp_posbias_add", "dp_posbias_sqnorm", "dp_posbias_workspace_bytes",
+           "dp_headnorm", "dp_headnorm_sqnorm", "dp_headnorm_workspace_bytes")
 
 # the measurement probes and plan queries of include/dpclip_probes.h
 PROBE_EXPORTS = ("dp_probe_mfma", "dp_probe_read", "dp_probe_lds_read", "dp_plan_gram_wide", "dp_plan_sums_in_two_lengths")
@@ -55,6 +56,22 @@ class PosbiasDesc(ctypes.Structure):
     _fields_ = ([(n, ctypes.c_int64) for n in ("B", "H", "Tq", "Tk", "s_b", "s_h", "s_q", "o_b", "o_h", "o_q")] +
                 [("buckets", ctypes.c_void_p), ("reach", ctypes.c_int64), ("n_buckets", ctypes.c_int64),
                  ("q_start", ctypes.c_void_p), ("q_lens", ctypes.c_void_p), ("k_lens", ctypes.c_void_p), ("causal", ctypes.c_int)])
+
+
+class HeadsDesc(ctypes.Structure):
+    """dp_heads_desc of the header."""
+    _fields_ = ([("x", ctypes.c_void_p), ("x_b", ctypes.c_int64), ("x_t", ctypes.c_int64), ("x_h", ctypes.c_int64),
+                 ("H", ctypes.c_int64), ("gain", ctypes.c_void_p),
+                 ("out", ctypes.c_void_p), ("o_b", ctypes.c_int64), ("o_t", ctypes.c_int64), ("o_h", ctypes.c_int64),
+                 ("dy", ctypes.c_void_p), ("dy_b", ctypes.c_int64), ("dy_t", ctypes.c_int64), ("dy_h", ctypes.c_int64),
+                 ("gain_rows", ctypes.c_void_p)])
+
+
+class HeadnormDesc(ctypes.Structure):
+    """dp_headnorm_desc of the header."""
+    _fields_ = [("B", ctypes.c_int64), ("T", ctypes.c_int64), ("D", ctypes.c_int64), ("rot", ctypes.c_int64),
+                ("rotation", ctypes.c_int), ("eps", ctypes.c_float), ("positions", ctypes.c_void_p),
+                ("positions_b", ctypes.c_int64), ("freqs", ctypes.c_void_p), ("lengths", ctypes.c_void_p)]
 
 
 class DpclipError(RuntimeError):
@@ -136,6 +153,12 @@ def load_library() -> ctypes.CDLL:
     lib.dp_posbias_sqnorm.restype = ci
     lib.dp_posbias_workspace_bytes.argtypes = [i64, i64, i64, i64]
     lib.dp_posbias_workspace_bytes.restype = sz
+    lib.dp_headnorm.argtypes = [ctypes.POINTER(HeadnormDesc), ctypes.POINTER(HeadsDesc), i64, ci, vp]
+    lib.dp_headnorm.restype = ci
+    lib.dp_headnorm_sqnorm.argtypes = [ctypes.POINTER(HeadnormDesc), ctypes.POINTER(HeadsDesc), i64, ci, ci, vp, vp, sz, vp]
+    lib.dp_headnorm_sqnorm.restype = ci
+    lib.dp_headnorm_workspace_bytes.argtypes = [i64, i64, i64, i64]
+    lib.dp_headnorm_workspace_bytes.restype = sz
     lib.dp_probe_mfma.argtypes = [ci, ci, i64, vp, ctypes.POINTER(ctypes.c_double), vp]
     lib.dp_probe_mfma.restype = ci
     lib.dp_probe_read.argtypes = [vp, sz, vp, vp]
@@ -859,6 +882,130 @@ def posbias_sqnorm(dS: torch.Tensor, buckets: torch.Tensor, n_buckets: int, sqno
                                _f32(rows, (B, n_buckets, H), "rows"), *_ws_args(ws), _stream_ptr(stream))
     _check(st, "dp_posbias_sqnorm")
     return sqnorm, rows
+
+
+class HeadDescs(NamedTuple):
+    arr: object                     # ctypes array of dp_heads_desc
+    device: torch.device
+    B: int
+    T: int
+    D: int
+    dtype: int
+    outs: list
+    gain_rows: Optional[list]
+
+
+def rotary_freqs(rot: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
+    """Angles per position of the rot / 2 pairs, base^(-2 j / rot), float64."""
+    return torch.tensor([float(base) ** (-2.0 * j / rot) for j in range(rot // 2)], dtype=torch.float64, device=device)
+
+
+def head_descs(heads, outs, dys=None, gain_rows=None) -> HeadDescs:
+    """Descriptors for headnorm (outs: its outputs) and with dys and gain_rows for headnorm_sqnorm (outs: the inputs' gradients).
+    heads: one or two (x, gain) pairs, queries and keys; x, outs and dys: [B, T, H, D] of one dtype, any strides but the last
+    dimension's; gain: float32 [D]; gain_rows: float32 [B, D].  The tensors must stay alive, and where they are, while the
+    descriptors are used."""
+    heads = list(heads)
+    if not 1 <= len(heads) <= 2 or len(outs) != len(heads) or (dys is not None and len(dys) != len(heads)):
+        raise ValueError("one or two (x, gain) pairs, with an output (and a gradient) each")
+    if (dys is None) != (gain_rows is None) or (gain_rows is not None and len(gain_rows) != len(heads)):
+        raise ValueError("dys and gain_rows go together")
+    arr = (HeadsDesc * len(heads))()
+    x0 = heads[0][0]
+    for i, (x, gain) in enumerate(heads):
+        xp, op = _inner(x, 4, "x"), _inner(outs[i], 4, "outs")
+        B, T, H, D = x.shape
+        if (B, T, D) != (x0.shape[0], x0.shape[1], x0.shape[3]) or x.dtype != x0.dtype:
+            raise ValueError("queries and keys must share batch, tokens, head size and dtype")
+        s, o, g, gp, rp = x.stride(), outs[i].stride(), (0, 0, 0), None, None
+        others = [outs[i], gain]
+        if dys is not None:
+            gp, g = _inner(dys[i], 4, "dys"), dys[i].stride()
+            rp = _f32(gain_rows[i], (B, D), "gain_rows")
+            others += [dys[i], gain_rows[i]]
+            if dys[i].shape != x.shape or dys[i].dtype != x.dtype:
+                raise ValueError("dys must have the shape and the dtype of x")
+        if outs[i].shape != x.shape or outs[i].dtype != x.dtype:
+            raise ValueError("outs must have the shape and the dtype of x")
+        if any(t.device != x0.device for t in (x, *others)):
+            raise ValueError("tensors must all be on one device")
+        arr[i] = HeadsDesc(xp, s[0], s[1], s[2], H, _f32(gain, (D,), "gain"), op, o[0], o[1], o[2], gp, g[0], g[1], g[2], rp)
+    return HeadDescs(arr, x0.device, x0.shape[0], x0.shape[1], x0.shape[3], _dtype_code(x0), list(outs),
+                     None if gain_rows is None else list(gain_rows))
+
+
+def _headnorm_desc(d: HeadDescs, freqs, positions, lengths, pairs, eps) -> HeadnormDesc:
+    rot = 0
+    if freqs is not None:
+        if not isinstance(freqs, torch.Tensor) or freqs.dtype != torch.float64 or not freqs.is_cuda or not freqs.is_contiguous() or freqs.dim() != 1:
+            raise TypeError("freqs must be a contiguous float64 device tensor of one dimension")
+        rot = 2 * freqs.numel()
+    pp, pb = None, 0
+    if positions is not None:
+        pb = d.T if positions.dim() == 2 else 0
+        pp = _i32(positions, d.B * d.T if positions.dim() == 2 else d.T, "positions")
+    return HeadnormDesc(d.B, d.T, d.D, rot, int(bool(pairs)), float(eps), pp, pb, freqs.data_ptr() if rot else None,
+                        _i32(lengths, d.B, "lengths"))
+
+
+def headnorm(heads, outs=None, *, freqs: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+             lengths: Optional[torch.Tensor] = None, pairs: bool = False, eps: float = 1e-6,
+             descs: Optional[HeadDescs] = None, stream: Optional[torch.cuda.Stream] = None):
+    """Every head of every token of one or two (x, gain) pairs, divided by the root of its mean square (plus eps), times the gain,
+    the pairs of its first 2 len(freqs) numbers turned by position * freqs[j], via dp_headnorm.  Returns the outputs.
+    heads, outs: as in head_descs (outs made if None, with zeros where lengths leave tokens out); freqs: float64, None for no rotation
+    (rotary_freqs makes the usual ones); positions: int32 [B, T] or [T], None for 0, 1, ...; pairs: neighbours turn together
+    instead of the halves' numbers; lengths: int32 [B], tokens from there on are left as they are in outs.
+    descs: the result of head_descs(heads, outs), to skip rebuilding it on every call."""
+    lib = load_library()
+    if descs is None:
+        with _made_on(stream):
+            if outs is None:
+                make = torch.empty if lengths is None else torch.zeros
+                outs = [make(x.shape, dtype=x.dtype, device=x.device) for x, _ in heads]
+        descs = head_descs(heads, outs)
+    _here(descs.device, stream, freqs, positions, lengths)
+    d = _headnorm_desc(descs, freqs, positions, lengths, pairs, eps)
+    st = lib.dp_headnorm(ctypes.byref(d), descs.arr, len(descs.arr), descs.dtype, _stream_ptr(stream))
+    _check(st, "dp_headnorm")
+    return descs.outs
+
+
+def headnorm_workspace_bytes(descs: HeadDescs) -> int:
+    return int(load_library().dp_headnorm_workspace_bytes(len(descs.arr), descs.B, descs.T, descs.D))
+
+
+def headnorm_sqnorm(heads, dys, sqnorm: Optional[torch.Tensor] = None, outs=None, gain_rows=None, *, accumulate: bool = False,
+                    freqs: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                    lengths: Optional[torch.Tensor] = None, pairs: bool = False, eps: float = 1e-6,
+                    workspace: Optional[torch.Tensor] = None, descs: Optional[HeadDescs] = None,
+                    stream: Optional[torch.cuda.Stream] = None):
+    """The backward pass of headnorm (same arguments) from the outputs' gradients dys, via dp_headnorm_sqnorm: the inputs'
+    gradients, the per-example gradients of the gains, gain_rows[i] = float32 [B, D], and sqnorm[b] (+)= their squared norms.
+    Returns (sqnorm, gain_rows, inputs' gradients); a gain's clipped sum is clipped_bias_grad(gain_rows[i], clip).
+    descs: the result of head_descs(heads, outs, dys, gain_rows)."""
+    lib = load_library()
+    if sqnorm is None and accumulate:
+        raise ValueError("accumulate needs an existing sqnorm tensor")
+    with _made_on(stream):
+        if descs is None:
+            if outs is None:
+                make = torch.empty if lengths is None else torch.zeros
+                outs = [make(x.shape, dtype=x.dtype, device=x.device) for x, _ in heads]
+            if gain_rows is None:
+                gain_rows = [torch.empty((x.shape[0], x.shape[-1]), dtype=torch.float32, device=x.device) for x, _ in heads]
+            descs = head_descs(heads, outs, dys, gain_rows)
+        elif descs.gain_rows is None:
+            raise ValueError("descs without gradients")
+        if sqnorm is None:
+            sqnorm = torch.empty(descs.B, dtype=torch.float32, device=descs.device)
+        ws = _workspace(lambda: headnorm_workspace_bytes(descs), descs.device, workspace)
+    _here(descs.device, stream, sqnorm, freqs, positions, lengths, workspace)
+    d = _headnorm_desc(descs, freqs, positions, lengths, pairs, eps)
+    st = lib.dp_headnorm_sqnorm(ctypes.byref(d), descs.arr, len(descs.arr), descs.dtype, int(bool(accumulate)),
+                                _f32(sqnorm, (descs.B,), "sqnorm"), *_ws_args(ws), _stream_ptr(stream))
+    _check(st, "dp_headnorm_sqnorm")
+    return sqnorm, descs.gain_rows, descs.outs
 
 
 def clipped_grad_rounds_inputs(B: int, T: int, d_in: int, d_out: int, dtype: int) -> bool:
