@@ -457,7 +457,7 @@ size_t dp_tensors_workspace_bytes(int64_t n_tensors);
  *     rows[b, j, h] = sum of dS[b, h, q, k] over the live (q, k) of bucket j.
  * Query q of example b stands at position q + q_start[b], key k at position k.  A
  * pair (q, k) is live if q < q_lens[b], k < k_lens[b] and, with `causal`, k <= q +
- * q_start[b]; what is not live is neither read nor written, whatever is there. */
+ * q_start[b]; what is not live counts for nothing and is not written, whatever is there. */
 typedef struct {
     int64_t B, H, Tq, Tk;
     int64_t s_b, s_h, s_q;     /* strides of the scores (or dS) in elements, >= 0; keys are next to each other */

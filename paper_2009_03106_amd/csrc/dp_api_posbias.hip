@@ -68,8 +68,7 @@ dp_status dp_posbias_sqnorm(const dp_posbias_desc* desc, const void* dS, dp_dtyp
     if (!dS || !rows || !d.buckets || !element_aligned(dS, dtype)) return DP_ERR_INVALID_ARG;
     if (width > INT32_MAX) return DP_ERR_UNSUPPORTED;
     if (!workspace || workspace_bytes < posbias_ws_bytes((int)d.B, (int)d.H, (int)d.Tq, (int)d.Tk) || ((uintptr_t)workspace & 15) != 0) return DP_ERR_WORKSPACE;
-    hipError_t e = launch_posbias_rows(args_of(d), dS, (int)dtype, rows, workspace, st);
-    if (e == hipSuccess) e = launch_rows_sqnorm(rows, (int)d.B, (int)width, accumulate != 0, sqnorm, st);
+    const hipError_t e = launch_posbias_sqnorm(args_of(d), dS, (int)dtype, accumulate != 0, rows, sqnorm, workspace, st);
     return e == hipSuccess ? DP_OK : DP_ERR_HIP;
 }
 

@@ -68,6 +68,73 @@ template <int DT> __device__ __forceinline__ void store8(void* p, int64_t k, con
     }
 }
 
+// The first n of eight elements, 0 < n < 8, in pieces of 4, 2 and 1: zeros behind them, and nothing behind them is touched.
+template <int DT, int N> __device__ __forceinline__ void load_piece(const void* p, int64_t k, float (&v)[N]) {
+    if constexpr (N == 1) {
+        v[0] = load_one<DT>(p, k);
+    } else if constexpr (DT == 0) {
+        typedef uint32_t piece __attribute__((ext_vector_type(N), aligned(4)));
+        const piece r = *global_in<piece>(static_cast<const float*>(p) + k);
+#pragma unroll
+        for (int j = 0; j < N; ++j) v[j] = __uint_as_float(r[j]);
+    } else if constexpr (N == 2) {
+        typedef uint32_t piece __attribute__((aligned(2)));
+        const uint32_t r = *global_in<piece>(static_cast<const uint16_t*>(p) + k);
+        v[0] = In16<DT == 2>::lo(r);
+        v[1] = In16<DT == 2>::hi(r);
+    } else {
+        typedef uint32_t piece __attribute__((ext_vector_type(N / 2), aligned(2)));
+        const piece r = *global_in<piece>(static_cast<const uint16_t*>(p) + k);
+#pragma unroll
+        for (int j = 0; j < N / 2; ++j) { v[2 * j] = In16<DT == 2>::lo(r[j]); v[2 * j + 1] = In16<DT == 2>::hi(r[j]); }
+    }
+}
+template <int DT, int N> __device__ __forceinline__ void store_piece(void* p, int64_t k, const float (&v)[N]) {
+    if constexpr (N == 1) {
+        store_one<DT>(p, k, v[0]);
+    } else if constexpr (DT == 0) {
+        typedef uint32_t piece __attribute__((ext_vector_type(N), aligned(4)));
+        piece r;
+#pragma unroll
+        for (int j = 0; j < N; ++j) r[j] = __float_as_uint(v[j]);
+        *global_out<piece>(static_cast<float*>(p) + k) = r;
+    } else if constexpr (N == 2) {
+        typedef uint32_t piece __attribute__((aligned(2)));
+        *global_out<piece>(static_cast<uint16_t*>(p) + k) = In16<DT == 2>::pack(v[0], v[1]);
+    } else {
+        typedef uint32_t piece __attribute__((ext_vector_type(N / 2), aligned(2)));
+        piece r;
+#pragma unroll
+        for (int j = 0; j < N / 2; ++j) r[j] = In16<DT == 2>::pack(v[2 * j], v[2 * j + 1]);
+        *global_out<piece>(static_cast<uint16_t*>(p) + k) = r;
+    }
+}
+template <int DT> __device__ __forceinline__ void load_first(const void* p, int64_t k, int n, float (&v)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = 0.f;
+    if (n & 4) { float f[4]; load_piece<DT>(p, k, f); v[0] = f[0]; v[1] = f[1]; v[2] = f[2]; v[3] = f[3]; }
+    if (n & 2) {
+        float f[2];
+        load_piece<DT>(p, k + (n & 4), f);
+        if (n & 4) { v[4] = f[0]; v[5] = f[1]; } else { v[0] = f[0]; v[1] = f[1]; }
+    }
+    if (n & 1) {
+        float f[1];
+        load_piece<DT>(p, k + (n & 6), f);
+#pragma unroll
+        for (int j = 0; j < 8; j += 2)
+            if ((n & 6) == j) v[j] = f[0];
+    }
+}
+template <int DT> __device__ __forceinline__ void store_first(void* p, int64_t k, int n, const float (&v)[8]) {
+    if (n & 4) { const float f[4] = {v[0], v[1], v[2], v[3]}; store_piece<DT>(p, k, f); }
+    if (n & 2) { const float f[2] = {n & 4 ? v[4] : v[0], n & 4 ? v[5] : v[1]}; store_piece<DT>(p, k + (n & 4), f); }
+    if (n & 1) {
+        const float f[1] = {n & 4 ? (n & 2 ? v[6] : v[4]) : (n & 2 ? v[2] : v[0])};
+        store_piece<DT>(p, k + (n & 6), f);
+    }
+}
+
 __device__ __forceinline__ double wave_sum_f64(double v) {
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, kWave);

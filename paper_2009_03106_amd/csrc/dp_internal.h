@@ -125,8 +125,7 @@ constexpr int kMaxBuckets = 1024;
 bool posbias_fits(int64_t B, int64_t H, int64_t Tq, int64_t Tk);       // what the launches below hold
 size_t posbias_ws_bytes(int B, int H, int Tq, int Tk);
 hipError_t launch_posbias_add(const PosbiasArgs& a, const void* scores, const float* table, int dt, void* out, hipStream_t st);
-// rows [B, n_buckets, H]; their norms are launch_rows_sqnorm's
-hipError_t launch_posbias_rows(const PosbiasArgs& a, const void* dS, int dt, float* rows, void* ws, hipStream_t st);
+hipError_t launch_posbias_sqnorm(const PosbiasArgs& a, const void* dS, int dt, bool accumulate, float* rows, float* sqnorm, void* ws, hipStream_t st);
 
 // ---- norms of queries and keys with the rotation (dp_headnorm.hip)
 struct HeadsArgs { const void* x; int64_t x_b, x_t, x_h; int H; const float* gain; void* out; int64_t o_b, o_t, o_h; const void* dy; int64_t dy_b, dy_t, dy_h; float* gain_rows; };

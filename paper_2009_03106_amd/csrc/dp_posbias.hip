@@ -43,56 +43,216 @@ __global__ __launch_bounds__(kThreads) void k_posbias_add(PosbiasArgs a, const v
     }
 }
 
-// Diagonal d of a head, 0 <= d < Tq + Tk - 1, holds the pairs with k - q = d - (Tq - 1).  A thread adds one up; the threads
-// of a wave have neighbouring ones, whose elements of a query are next to each other.
+// ---- the gradient
+// A lane adds up blocks of 8 queries x 8 keys along a diagonal of blocks: block (rb, rb + m) for one m and rb = r0, r0 + 1, ...
+// All of them have their elements on the same 15 diagonals, k - q = 8 m + e with -7 <= e <= 7, so the sums stay in the lane's
+// registers, and a group of LC lanes with neighbouring m reads LC pieces of 16 bytes (8 of float32: 32) next to each other
+// of every query.  The diagonal of a block is added in float32 (at most 8 elements), the blocks in 64 bits.
+// A thread per diagonal, one element after the other in 64 bits, took 2950 us for 64 x 12 x 512 x 512 bf16; see the table of
+// measurements at launch_posbias_rows.
+struct Walk {
+    int lc;                    // log2 of LC
+    int R, C;                  // blocks of queries, of keys
+    int m_first, bands;        // bands of LC diagonals of blocks, from m_first on
+    int segs;                  // pieces that a band's rows of blocks are cut into
+    int wgs;                   // workgroups of an example's head; a group of lanes has one piece of one band
+};
+constexpr int kMaxSlots = kThreads * 8 + 8 * (kThreads / 8);
+
 template <int DT>
-__global__ __launch_bounds__(kThreads) void k_posbias_diagonals(PosbiasArgs a, const void* __restrict__ dS, int diagonals, int pieces, double* __restrict__ sums) {
-    const int bh = blockIdx.x / pieces, h = bh % a.H, b = bh / a.H;
-    const int d = (blockIdx.x % pieces) * kThreads + threadIdx.x;
-    if (d >= diagonals) return;
+__global__ __launch_bounds__(kThreads, 3) void k_posbias_walk(PosbiasArgs a, const void* __restrict__ dS, Walk wk, double* __restrict__ partial, float* __restrict__ rows) {
+    __shared__ double val[kMaxSlots];                  // [groups][8 LC + 8]: sums of the groups' diagonals
+    __shared__ short bkt[kMaxSlots];                   // and their buckets
+    const int tid = threadIdx.x, LC = 1 << wk.lc, G = kThreads >> wk.lc, P = 8 * LC + 8;
+    const int li = tid & (LC - 1), g = tid >> wk.lc;
+    const int wg = blockIdx.x % wk.wgs, bh = blockIdx.x / wk.wgs, h = bh % a.H, b = bh / a.H;
     const Window w = window_of(a, b);
-    const int off = d - (a.Tq - 1);
-    double acc = 0.0;
-    if (!a.causal || off <= w.start) {
-        const int64_t base = b * a.s_b + h * a.s_h + off;
-        const int last = min(w.nq, w.nk - off);
-        for (int q = max(0, -off); q < last; ++q) acc += load_one<DT>(dS, base + q * (a.s_q + 1));
+    const int task = wg * G + g, band = task / wk.segs, seg = task - band * wk.segs;
+    const int m0 = wk.m_first + band * LC, m = m0 + li;
+    double acc[15];
+#pragma unroll
+    for (int e = 0; e < 15; ++e) acc[e] = 0.0;
+    if (band < wk.bands) {
+        const int lo = max(0, -(m0 + LC - 1)), hi = min(min(wk.R, (w.nq + 7) / 8), wk.C - m0), len = max(0, hi - lo);
+        const int r0 = lo + (int)((int64_t)len * seg / wk.segs), r1 = lo + (int)((int64_t)len * (seg + 1) / wk.segs);
+        const int64_t base = b * a.s_b + h * a.s_h;
+        const bool narrow = a.Tk < 8;
+        const int over = wk.C * 8 - a.Tk;              // how far the last block of keys reaches beyond the row
+        for (int rb = r0; rb < r1; ++rb) {
+            const int q0 = rb * 8, k0 = (rb + m) * 8, nk = min(8, w.nk - k0), nq = min(8, w.nq - q0);
+            // no live element: left of the first key, behind the last one, all keys behind the queries
+            if (rb + m < 0 || nk <= 0 || (a.causal && (int64_t)k0 - (q0 + 7) > w.start)) continue;
+            float d[15];
+#pragma unroll
+            for (int e = 0; e < 15; ++e) d[e] = 0.f;
+            if (narrow) {                              // rows shorter than a piece
+                for (int i = 0; i < nq; ++i) {
+                    float v[8];
+                    load_first<DT>(dS, base + (q0 + i) * a.s_q, nk, v);
+#pragma unroll
+                    for (int y = 0; y < 8; ++y)
+                        if (y == i)
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) d[7 + j - y] += v[j];
+                }
+            } else {
+                // 128 bytes at once, all of them within the tensor: the last keys' pieces begin `over` earlier, queries behind the
+                // last one are the last one again
+                constexpr int kAtOnce = DT == 0 ? 4 : 8;
+                const bool last = k0 + 8 > a.Tk;
+                const int64_t at = base + q0 * a.s_q + (last ? k0 - over : k0), last_row = (a.Tq - 1 - q0) * a.s_q;
+                const bool whole = __ballot(nk < 8 || nq < 8) == 0;
+#pragma unroll
+                for (int i0 = 0; i0 < 8; i0 += kAtOnce) {
+                    Raw8<DT> r[kAtOnce];
+#pragma unroll
+                    for (int i = 0; i < kAtOnce; ++i) r[i] = load_raw8<DT>(dS, at + min((i0 + i) * a.s_q, last_row));
+                    if (whole) {
+#pragma unroll
+                        for (int i = 0; i < kAtOnce; ++i) {
+                            float v[8];
+                            widen8<DT>(r[i], v);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) d[7 + j - i0 - i] += v[j];
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < kAtOnce; ++i) {
+                            float v[8];
+                            widen8<DT>(r[i], v);
+                            if (over & 4)
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) v[j] = last ? v[j + 4] : v[j];
+                            if (over & 2)
+#pragma unroll
+                                for (int j = 0; j < 6; ++j) v[j] = last ? v[j + 2] : v[j];
+                            if (over & 1)
+#pragma unroll
+                                for (int j = 0; j < 7; ++j) v[j] = last ? v[j + 1] : v[j];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) d[7 + j - i0 - i] += j < nk && i0 + i < nq ? v[j] : 0.f;
+                        }
+                    }
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 15; ++e) acc[e] += d[e];
+        }
     }
-    sums[(int64_t)bh * diagonals + d] = acc;
+    // lane li's diagonals are slots 8 li ... 8 li + 14 of its group: the upper seven are the next lane's too
+#pragma unroll
+    for (int y = 0; y < 7; ++y) {
+        const double left = __shfl_up(acc[y + 8], 1, LC);
+        if (li > 0) acc[y] += left;
+    }
+    double* v = val + g * P + 8 * li;
+#pragma unroll
+    for (int y = 0; y < 8; ++y) v[y] = acc[y];
+    if (li == LC - 1) {
+#pragma unroll
+        for (int y = 0; y < 7; ++y) v[8 + y] = acc[8 + y];
+        v[15] = 0.0;
+    }
+    // the pieces of a band are added: a slot per diagonal of each band that this workgroup has a piece of
+    const int t0 = wg * G, first = t0 / wk.segs, slots = (min(wk.bands - 1, (t0 + G - 1) / wk.segs) - first + 1) * P;
+    __syncthreads();
+    double sum[kMaxSlots / kThreads];
+#pragma unroll
+    for (int i = 0; i < kMaxSlots / kThreads; ++i) {
+        const int s = tid + i * kThreads, bd = first + s / P, x = s % P;
+        double v = 0.0;
+        if (s < slots) {
+            const int end = min((bd + 1) * wk.segs - t0, G);
+            for (int t = max(bd * wk.segs - t0, 0); t < end; ++t) v += val[t * P + x];
+            const int64_t distance = (int64_t)8 * (wk.m_first + bd * LC) + x - 7 - w.start;
+            const int j = a.causal && distance > 0 ? -1 : bucket_of(a, distance);
+            bkt[s] = (short)(j >= 0 && j < a.n_buckets ? j : -1);
+        }
+        sum[i] = v;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kMaxSlots / kThreads; ++i)
+        if (tid + i * kThreads < slots) val[tid + i * kThreads] = sum[i];
+    __syncthreads();
+    // 2^ul threads for a bucket look through all slots
+    int ul = 6;
+    while (ul > 0 && (kThreads >> ul) < a.n_buckets) --ul;
+    const int u = tid & ((1 << ul) - 1);
+    for (int j0 = 0; j0 < a.n_buckets; j0 += kThreads >> ul) {
+        const int j = j0 + (tid >> ul);
+        double s = 0.0;
+        int k = u;
+        for (; k + (7 << ul) < slots; k += 8 << ul) {
+            double v[8];
+            int c[8];
+#pragma unroll
+            for (int y = 0; y < 8; ++y) { v[y] = val[k + (y << ul)]; c[y] = bkt[k + (y << ul)]; }
+#pragma unroll
+            for (int y = 0; y < 8; ++y) s += c[y] == j ? v[y] : 0.0;
+        }
+        for (; k < slots; k += 1 << ul) s += bkt[k] == j ? val[k] : 0.0;
+        for (int off = 1; off < 1 << ul; off <<= 1) s += __shfl_xor(s, off, kWave);
+        if (u == 0 && j < a.n_buckets) {
+            if (wk.wgs == 1) rows[((int64_t)b * a.n_buckets + j) * a.H + h] = (float)s;
+            else             partial[(int64_t)blockIdx.x * a.n_buckets + j] = s;
+        }
+    }
 }
 
-// A workgroup per example and head: the diagonals' sums by buckets.  The lanes of a wave that share a bucket are added by the
-// wave, one bucket after the other, into the wave's own sums: a fixed order.
-__global__ __launch_bounds__(kThreads) void k_posbias_fold(PosbiasArgs a, const double* __restrict__ sums, int diagonals, float* __restrict__ rows) {
-    extern __shared__ double acc[];                    // [waves][n_buckets]
-    constexpr int kWaves = kThreads / kWave;
-    const int bh = blockIdx.x, h = bh % a.H, b = bh / a.H, wave = threadIdx.x >> 6, lane = threadIdx.x & (kWave - 1);
-    for (int j = threadIdx.x; j < kWaves * a.n_buckets; j += kThreads) acc[j] = 0.0;
-    __syncthreads();
-    const Window w = window_of(a, b);
-    for (int d0 = wave * kWave; d0 < diagonals; d0 += kThreads) {
-        const int d = d0 + lane;
-        int j = -1;
-        double v = 0.0;
-        if (d < diagonals) {
-            v = sums[(int64_t)bh * diagonals + d];
-            j = bucket_of(a, (int64_t)d - (a.Tq - 1) - w.start);
-            if (j >= a.n_buckets) j = -1;
-        }
-        for (uint64_t left = __ballot(j >= 0); left;) {
-            const int one = __builtin_amdgcn_readlane(j, (int)__builtin_ctzll(left));
-            const double s = wave_sum_f64(j == one ? v : 0.0);
-            if (lane == 0) acc[wave * a.n_buckets + one] += s;
-            left &= ~__ballot(j == one);
-        }
-    }
-    __syncthreads();
-    for (int j = threadIdx.x; j < a.n_buckets; j += kThreads) {
-        double s = acc[j];
+// A workgroup per example: the sums of its heads' workgroups where there are several, and the squared norm of the rows.
+constexpr int kFinishThreads = 1024;
+__global__ __launch_bounds__(kFinishThreads) void k_posbias_finish(PosbiasArgs a, int wgs, const double* __restrict__ partial, int accumulate, float* __restrict__ rows, float* __restrict__ sqnorm) {
+    __shared__ double red[kFinishThreads / kWave];
+    const int b = blockIdx.x, n = a.n_buckets * a.H;
+    float* r = rows + (int64_t)b * n;
+    double sq = 0.0;
+    if (wgs == 1) {
+        for (int k = threadIdx.x; k < n; k += kFinishThreads) sq += (double)r[k] * r[k];
+    } else {
+        for (int k = threadIdx.x; k < n; k += kFinishThreads) {          // neighbouring threads: neighbouring buckets
+            const int h = k / a.n_buckets, j = k - h * a.n_buckets;
+            const double* p = partial + ((int64_t)(b * (int64_t)a.H + h) * wgs) * a.n_buckets + j;
+            double s = 0.0;
+            int i = 0;
+            for (; i + 7 < wgs; i += 8) {
+                double v[8];
 #pragma unroll
-        for (int k = 1; k < kWaves; ++k) s += acc[k * a.n_buckets + j];
-        rows[((int64_t)b * a.n_buckets + j) * a.H + h] = (float)s;
+                for (int x = 0; x < 8; ++x) v[x] = p[(int64_t)(i + x) * a.n_buckets];
+#pragma unroll
+                for (int x = 0; x < 8; ++x) s += v[x];
+            }
+            for (; i < wgs; ++i) s += p[(int64_t)i * a.n_buckets];
+            const float f = (float)s;
+            r[(int64_t)j * a.H + h] = f;
+            sq += (double)f * f;
+        }
     }
+    sq = wave_sum_f64(sq);
+    if ((threadIdx.x & (kWave - 1)) == 0) red[threadIdx.x >> 6] = sq;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+#pragma unroll
+    for (int k = 1; k < kFinishThreads / kWave; ++k) sq += red[k];
+    sqnorm[b] = (float)(accumulate ? sqnorm[b] + sq : sq);
+}
+
+// How the blocks of a head are dealt.  Known keys behind every query (causal and no start of its own) get no bands.
+Walk plan_walk(int64_t BH, int Tq, int Tk, bool half) {
+    Walk w{};
+    w.R = (Tq + 7) / 8;
+    w.C = (Tk + 7) / 8;
+    w.m_first = -(w.R - 1);
+    const int diagonals = half ? w.R - 1 + std::min(1, w.C) : w.R + w.C - 1;
+    w.lc = 3;
+    while (w.lc < 5 && (1 << w.lc) < std::min(w.C, diagonals)) ++w.lc;
+    const int LC = 1 << w.lc, G = kThreads / LC;
+    w.bands = (diagonals + LC - 1) / LC;
+    // about eight workgroups for each of the 256 compute units, of pieces of at least four blocks
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>((2048 + BH - 1) / BH, ((int64_t)w.bands * ((w.R + 3) / 4) + G - 1) / G));
+    w.segs = (int)std::max<int64_t>(1, want * G / w.bands);
+    w.wgs = (int)(((int64_t)w.bands * w.segs + G - 1) / G);
+    return w;
 }
 
 }  // namespace
@@ -102,10 +262,16 @@ bool posbias_fits(int64_t B, int64_t H, int64_t Tq, int64_t Tk) {
     if (B >= most || H >= most || Tq >= most / 2 || Tk >= most / 2) return false;
     if (B == 0 || H == 0 || Tq == 0 || Tk == 0) return true;
     if (H > most / B || Tq > most / (B * H)) return false;
-    const int64_t pieces_add = (Tk + kThreads - 1) / kThreads, pieces = (Tq + Tk - 1 + kThreads - 1) / kThreads;
-    return launch_holds(B * H * ((Tq + kAddRows - 1) / kAddRows) * pieces_add, kThreads) && launch_holds(B * H * pieces, kThreads);
+    const int64_t pieces_add = (Tk + kThreads - 1) / kThreads;
+    return launch_holds(B * H * ((Tq + kAddRows - 1) / kAddRows) * pieces_add, kThreads)
+        && B < 1 << 22 && launch_holds(B * H * plan_walk(B * H, (int)Tq, (int)Tk, false).wgs, kThreads);
 }
-size_t posbias_ws_bytes(int B, int H, int Tq, int Tk) { return (size_t)B * H * ((size_t)Tq + Tk - 1) * sizeof(double); }
+// the sums of every workgroup, where a head has several; whether keys are left out is not known here
+size_t posbias_ws_bytes(int B, int H, int Tq, int Tk) {
+    const int64_t BH = (int64_t)B * H;
+    const int wgs = std::max(plan_walk(BH, Tq, Tk, false).wgs, plan_walk(BH, Tq, Tk, true).wgs);
+    return wgs > 1 ? (size_t)BH * wgs * kMaxBuckets * sizeof(double) : 16;
+}
 
 hipError_t launch_posbias_add(const PosbiasArgs& a, const void* scores, const float* table, int dt, void* out, hipStream_t st) {
     const int pieces = ceil_div(a.Tk, kThreads);
@@ -117,16 +283,17 @@ hipError_t launch_posbias_add(const PosbiasArgs& a, const void* scores, const fl
     return hipGetLastError();
 }
 
-hipError_t launch_posbias_rows(const PosbiasArgs& a, const void* dS, int dt, float* rows, void* ws, hipStream_t st) {
-    const int diagonals = a.Tq + a.Tk - 1, pieces = ceil_div(diagonals, kThreads);
-    const unsigned grid = (unsigned)((int64_t)a.B * a.H * pieces);
-    double* sums = static_cast<double*>(ws);
-    if (dt == 0)      k_posbias_diagonals<0><<<grid, kThreads, 0, st>>>(a, dS, diagonals, pieces, sums);
-    else if (dt == 1) k_posbias_diagonals<1><<<grid, kThreads, 0, st>>>(a, dS, diagonals, pieces, sums);
-    else              k_posbias_diagonals<2><<<grid, kThreads, 0, st>>>(a, dS, diagonals, pieces, sums);
+hipError_t launch_posbias_sqnorm(const PosbiasArgs& a, const void* dS, int dt, bool accumulate, float* rows, float* sqnorm, void* ws, hipStream_t st) {
+    const int64_t BH = (int64_t)a.B * a.H;
+    const Walk w = plan_walk(BH, a.Tq, a.Tk, a.causal && !a.q_start);
+    const unsigned grid = (unsigned)(BH * w.wgs);
+    double* partial = static_cast<double*>(ws);
+    if (dt == 0)      k_posbias_walk<0><<<grid, kThreads, 0, st>>>(a, dS, w, partial, rows);
+    else if (dt == 1) k_posbias_walk<1><<<grid, kThreads, 0, st>>>(a, dS, w, partial, rows);
+    else              k_posbias_walk<2><<<grid, kThreads, 0, st>>>(a, dS, w, partial, rows);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    k_posbias_fold<<<a.B * a.H, kThreads, (size_t)(kThreads / kWave) * a.n_buckets * sizeof(double), st>>>(a, sums, diagonals, rows);
+    k_posbias_finish<<<a.B, kFinishThreads, 0, st>>>(a, w.wgs, partial, accumulate, rows, sqnorm);
     return hipGetLastError();
 }
 
