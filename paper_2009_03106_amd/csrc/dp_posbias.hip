@@ -24,23 +24,93 @@ __device__ __forceinline__ int bucket_of(const PosbiasArgs& a, int64_t distance)
     return a.buckets[min(max(distance, -reach), reach) + reach];
 }
 
-// A workgroup per piece of 256 keys of eight queries.
-constexpr int kAddRows = 8;
+// ---- adding
+// A thread adds to blocks of 8 queries x 8 keys: eight loads of 16 bytes (float32: 32), 15 biases, eight stores.  A workgroup has
+// CT threads next to each other along the keys and RG along the queries, for `steps` rows of blocks each, and keeps the biases
+// of all its distances in LDS, so that the two dependent look-ups are made once for a distance and not once for an element.
+// One element after the other, with both look-ups, took 172 us for 32 x 12 x 512 x 512 bf16.
+struct AddTiles { int ct, rg, steps, row_tiles, col_tiles; };      // ct, rg: logarithms
+constexpr int kAddSteps = 8;
+constexpr int kAddDistances = 8 * (kThreads + kAddSteps);          // 8 (CT + RG steps) with CT RG = 256 threads
 template <int DT>
-__global__ __launch_bounds__(kThreads) void k_posbias_add(PosbiasArgs a, const void* scores, const float* __restrict__ table, void* out, int pieces, int row_blocks) {
-    const int piece = blockIdx.x % pieces, rb = blockIdx.x / pieces;
-    const int q0 = rb % row_blocks * kAddRows, bh = rb / row_blocks, h = bh % a.H, b = bh / a.H;
+__global__ __launch_bounds__(kThreads) void k_posbias_add(PosbiasArgs a, const void* scores, const float* __restrict__ table, void* out, AddTiles tl) {
+    __shared__ __align__(16) float bias[kAddDistances];
+    const int CT = 1 << tl.ct, RG = 1 << tl.rg;
+    const int tile = blockIdx.x % (tl.row_tiles * tl.col_tiles), bh = blockIdx.x / (tl.row_tiles * tl.col_tiles), h = bh % a.H, b = bh / a.H;
+    const int col0 = tile % tl.col_tiles * CT, row0 = tile / tl.col_tiles * RG * tl.steps;       // in blocks
     const Window w = window_of(a, b);
-    const int k = piece * kThreads + threadIdx.x;
-    if (k >= w.nk) return;
-    for (int q = q0; q < min(q0 + kAddRows, w.nq); ++q) {
-        const int64_t distance = (int64_t)k - q - w.start;
-        if (a.causal && distance > 0) continue;
-        const int j = bucket_of(a, distance);
-        const float bias = j >= 0 && j < a.n_buckets ? table[j * a.H + h] : 0.f;
-        const float s = load_one<DT>(scores, b * a.s_b + h * a.s_h + q * a.s_q + k);
-        store_one<DT>(out, b * a.o_b + h * a.o_h + q * a.o_q + k, s + bias);
+    // the distances k - q of the tile: from the first key and the last query on
+    const int64_t least = (int64_t)8 * col0 - (8 * ((int64_t)row0 + RG * tl.steps) - 1) - w.start;
+    if (8 * row0 >= w.nq || 8 * col0 >= w.nk || (a.causal && least > 0)) return;
+    for (int t = threadIdx.x; t < 8 * (CT + RG * tl.steps); t += kThreads) {
+        const int j = bucket_of(a, least + t);
+        bias[t] = j >= 0 && j < a.n_buckets ? table[j * a.H + h] : 0.f;
     }
+    __syncthreads();
+    const int ct = threadIdx.x & (CT - 1), rg = threadIdx.x >> tl.ct;
+    const int k0 = (col0 + ct) * 8, nk = min(8, w.nk - k0);
+    if (nk <= 0) return;
+    // every load lies within the tensor: those of the last keys begin `over` earlier (rows of at least 8 keys)
+    const bool narrow = a.Tk < 8, last = k0 + 8 > a.Tk;
+    const int over = (a.Tk + 7) / 8 * 8 - a.Tk;
+    const int64_t in0 = b * a.s_b + h * a.s_h + (last && !narrow ? k0 - over : k0), out0 = b * a.o_b + h * a.o_h + k0;
+    for (int s = 0; s < tl.steps; ++s) {
+        const int q0 = (row0 + s * RG + rg) * 8, nq = min(8, w.nq - q0);
+        if (nq <= 0) break;
+        if (a.causal && (int64_t)k0 - (q0 + 7) > w.start) continue;
+        float c[16];                                   // c[7 + j - i]: the bias of key j and query i of the block
+        const float4* cp = reinterpret_cast<const float4*>(bias + 8 * (ct + RG * tl.steps - 1 - (s * RG + rg)));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { const float4 f = cp[i]; c[4 * i] = f.x; c[4 * i + 1] = f.y; c[4 * i + 2] = f.z; c[4 * i + 3] = f.w; }
+        Raw8<DT> r[8];
+        if (!narrow) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < nq) r[i] = load_raw8<DT>(scores, in0 + (q0 + i) * a.s_q);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (i >= nq) break;
+            float v[8];
+            if (narrow) {
+                load_first<DT>(scores, in0 + (q0 + i) * a.s_q, nk, v);
+            } else {
+                widen8<DT>(r[i], v);
+                if (over & 4)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] = last ? v[j + 4] : v[j];
+                if (over & 2)
+#pragma unroll
+                    for (int j = 0; j < 6; ++j) v[j] = last ? v[j + 2] : v[j];
+                if (over & 1)
+#pragma unroll
+                    for (int j = 0; j < 7; ++j) v[j] = last ? v[j + 1] : v[j];
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += c[7 + j - i];
+            // the live keys of a query are its first ones
+            const int n = a.causal ? (int)min((int64_t)nk, max((int64_t)0, q0 + i + w.start - k0 + 1)) : nk;
+            const int64_t to = out0 + (q0 + i) * a.o_q;
+            if (n == 8) store8<DT>(out, to, v);
+            else        store_first<DT>(out, to, n, v);
+        }
+    }
+}
+
+// As many threads along the keys as there are blocks (a row's accesses are then next to each other), up to the whole workgroup;
+// rows of blocks one after the other while there are more than eight workgroups for each of the 256 compute units.
+AddTiles plan_add(int64_t BH, int Tq, int Tk) {
+    AddTiles t{};
+    const int R = (Tq + 7) / 8, C = (Tk + 7) / 8;
+    t.ct = 3;
+    while (t.ct < 8 && (1 << t.ct) < C) ++t.ct;
+    t.rg = 8 - t.ct;
+    t.col_tiles = (C + (1 << t.ct) - 1) >> t.ct;
+    const auto tiles = [&](int steps) { return (R + (steps << t.rg) - 1) / (steps << t.rg); };
+    t.steps = 1;
+    while (t.steps < kAddSteps && BH * t.col_tiles * tiles(2 * t.steps) >= 2048) t.steps *= 2;
+    t.row_tiles = tiles(t.steps);
+    return t;
 }
 
 // ---- the gradient
@@ -262,9 +332,9 @@ bool posbias_fits(int64_t B, int64_t H, int64_t Tq, int64_t Tk) {
     if (B >= most || H >= most || Tq >= most / 2 || Tk >= most / 2) return false;
     if (B == 0 || H == 0 || Tq == 0 || Tk == 0) return true;
     if (H > most / B || Tq > most / (B * H)) return false;
-    const int64_t pieces_add = (Tk + kThreads - 1) / kThreads;
-    return launch_holds(B * H * ((Tq + kAddRows - 1) / kAddRows) * pieces_add, kThreads)
-        && B < 1 << 22 && launch_holds(B * H * plan_walk(B * H, (int)Tq, (int)Tk, false).wgs, kThreads);
+    const AddTiles t = plan_add(B * H, (int)Tq, (int)Tk);
+    return launch_holds(B * H * t.row_tiles * t.col_tiles, kThreads)
+        && B < 1 << 22 && launch_holds(B * H * plan_walk(B * H, (int)Tq, (int)Tk, false).wgs, kThreads) && launch_holds(B * H * plan_walk(B * H, (int)Tq, (int)Tk, true).wgs, kThreads);
 }
 // the sums of every workgroup, where a head has several; whether keys are left out is not known here
 size_t posbias_ws_bytes(int B, int H, int Tq, int Tk) {
@@ -274,12 +344,11 @@ size_t posbias_ws_bytes(int B, int H, int Tq, int Tk) {
 }
 
 hipError_t launch_posbias_add(const PosbiasArgs& a, const void* scores, const float* table, int dt, void* out, hipStream_t st) {
-    const int pieces = ceil_div(a.Tk, kThreads);
-    const int row_blocks = ceil_div(a.Tq, kAddRows);
-    const unsigned grid = (unsigned)((int64_t)a.B * a.H * row_blocks * pieces);
-    if (dt == 0)      k_posbias_add<0><<<grid, kThreads, 0, st>>>(a, scores, table, out, pieces, row_blocks);
-    else if (dt == 1) k_posbias_add<1><<<grid, kThreads, 0, st>>>(a, scores, table, out, pieces, row_blocks);
-    else              k_posbias_add<2><<<grid, kThreads, 0, st>>>(a, scores, table, out, pieces, row_blocks);
+    const AddTiles t = plan_add((int64_t)a.B * a.H, a.Tq, a.Tk);
+    const unsigned grid = (unsigned)((int64_t)a.B * a.H * t.row_tiles * t.col_tiles);
+    if (dt == 0)      k_posbias_add<0><<<grid, kThreads, 0, st>>>(a, scores, table, out, t);
+    else if (dt == 1) k_posbias_add<1><<<grid, kThreads, 0, st>>>(a, scores, table, out, t);
+    else              k_posbias_add<2><<<grid, kThreads, 0, st>>>(a, scores, table, out, t);
     return hipGetLastError();
 }
 
