@@ -116,7 +116,9 @@ template <int DT> __device__ __forceinline__ void load_first(const void* p, int6
     if (n & 2) {
         float f[2];
         load_piece<DT>(p, k + (n & 4), f);
-        if (n & 4) { v[4] = f[0]; v[5] = f[1]; } else { v[0] = f[0]; v[1] = f[1]; }
+        const bool up = n & 4;
+        v[4] = up ? f[0] : 0.f; v[5] = up ? f[1] : 0.f;
+        v[0] = up ? v[0] : f[0]; v[1] = up ? v[1] : f[1];
     }
     if (n & 1) {
         float f[1];
@@ -126,13 +128,24 @@ template <int DT> __device__ __forceinline__ void load_first(const void* p, int6
             if ((n & 6) == j) v[j] = f[0];
     }
 }
-template <int DT> __device__ __forceinline__ void store_first(void* p, int64_t k, int n, const float (&v)[8]) {
-    if (n & 4) { const float f[4] = {v[0], v[1], v[2], v[3]}; store_piece<DT>(p, k, f); }
-    if (n & 2) { const float f[2] = {n & 4 ? v[4] : v[0], n & 4 ? v[5] : v[1]}; store_piece<DT>(p, k + (n & 4), f); }
-    if (n & 1) {
-        const float f[1] = {n & 4 ? (n & 2 ? v[6] : v[4]) : (n & 2 ? v[2] : v[0])};
-        store_piece<DT>(p, k + (n & 6), f);
+// (The elements go by value: with an array behind a reference the compiler joins the branches' stores into one of an element by
+// index, and gives the array a place in scratch memory or in LDS.  For LDS it reads the workgroup's size from the dispatch packet,
+// in host memory: 13 us for a launch.)
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+template <int DT> __device__ __forceinline__ void store_first(void* p, int64_t k, int n, f32x8 v) {
+    if (n & 4) {
+        const float f[4] = {v[0], v[1], v[2], v[3]};
+        store_piece<DT>(p, k, f);
+        v = __builtin_shufflevector(v, v, 4, 5, 6, 7, 4, 5, 6, 7);
+        k += 4;
     }
+    if (n & 2) {
+        const float f[2] = {v[0], v[1]};
+        store_piece<DT>(p, k, f);
+        v = __builtin_shufflevector(v, v, 2, 3, 2, 3, 2, 3, 2, 3);
+        k += 2;
+    }
+    if (n & 1) store_one<DT>(p, k, v[0]);
 }
 
 __device__ __forceinline__ double wave_sum_f64(double v) {

@@ -25,10 +25,10 @@ __device__ __forceinline__ int bucket_of(const PosbiasArgs& a, int64_t distance)
 }
 
 // ---- adding
-// A thread adds to blocks of 8 queries x 8 keys: eight loads of 16 bytes (float32: 32), 15 biases, eight stores.  A workgroup has
-// CT threads next to each other along the keys and RG along the queries, for `steps` rows of blocks each, and keeps the biases
-// of all its distances in LDS, so that the two dependent look-ups are made once for a distance and not once for an element.
-// One element after the other, with both look-ups, took 172 us for 32 x 12 x 512 x 512 bf16.
+// A thread adds to blocks of 8 queries x 8 keys, four queries at a time: four loads of 16 bytes (float32: 32), 11 biases, four
+// stores.  A workgroup has CT threads next to each other along the keys and RG along the queries, for `steps` rows of blocks
+// each, and keeps the biases of all its distances in LDS, so that the two dependent look-ups are made once for a distance and
+// not once for an element.  One element after the other, with both look-ups, took 172 us for 32 x 12 x 512 x 512 bf16.
 struct AddTiles { int ct, rg, steps, row_tiles, col_tiles; };      // ct, rg: logarithms
 constexpr int kAddSteps = 8;
 constexpr int kAddDistances = 8 * (kThreads + kAddSteps);          // 8 (CT + RG steps) with CT RG = 256 threads
@@ -42,57 +42,67 @@ __global__ __launch_bounds__(kThreads) void k_posbias_add(PosbiasArgs a, const v
     // the distances k - q of the tile: from the first key and the last query on
     const int64_t least = (int64_t)8 * col0 - (8 * ((int64_t)row0 + RG * tl.steps) - 1) - w.start;
     if (8 * row0 >= w.nq || 8 * col0 >= w.nk || (a.causal && least > 0)) return;
-    for (int t = threadIdx.x; t < 8 * (CT + RG * tl.steps); t += kThreads) {
-        const int j = bucket_of(a, least + t);
-        bias[t] = j >= 0 && j < a.n_buckets ? table[j * a.H + h] : 0.f;
-    }
-    __syncthreads();
     const int ct = threadIdx.x & (CT - 1), rg = threadIdx.x >> tl.ct;
     const int k0 = (col0 + ct) * 8, nk = min(8, w.nk - k0);
-    if (nk <= 0) return;
     // every load lies within the tensor: those of the last keys begin `over` earlier (rows of at least 8 keys)
     const bool narrow = a.Tk < 8, last = k0 + 8 > a.Tk;
     const int over = (a.Tk + 7) / 8 * 8 - a.Tk;
     const int64_t in0 = b * a.s_b + h * a.s_h + (last && !narrow ? k0 - over : k0), out0 = b * a.o_b + h * a.o_h + k0;
-    for (int s = 0; s < tl.steps; ++s) {
-        const int q0 = (row0 + s * RG + rg) * 8, nq = min(8, w.nq - q0);
+    const int distances = 8 * (CT + RG * tl.steps);
+    for (int t0 = threadIdx.x; t0 < distances; t0 += 4 * kThreads) {
+        int j[4];
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) j[i] = bucket_of(a, least + t0 + i * kThreads);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = j[i] >= 0 && j[i] < a.n_buckets ? table[j[i] * a.H + h] : 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (t0 + i * kThreads < distances) bias[t0 + i * kThreads] = v[i];
+    }
+    __syncthreads();
+    if (nk <= 0) return;
+#pragma unroll 1
+    for (int s = 0; s < 2 * tl.steps; ++s) {
+        const int block = (s >> 1) * RG + rg, half = 4 * (s & 1), q0 = (row0 + block) * 8 + half, nq = min(4, w.nq - q0);
         if (nq <= 0) break;
-        if (a.causal && (int64_t)k0 - (q0 + 7) > w.start) continue;
-        float c[16];                                   // c[7 + j - i]: the bias of key j and query i of the block
-        const float4* cp = reinterpret_cast<const float4*>(bias + 8 * (ct + RG * tl.steps - 1 - (s * RG + rg)));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { const float4 f = cp[i]; c[4 * i] = f.x; c[4 * i + 1] = f.y; c[4 * i + 2] = f.z; c[4 * i + 3] = f.w; }
-        Raw8<DT> r[8];
-        if (!narrow) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < nq) r[i] = load_raw8<DT>(scores, in0 + (q0 + i) * a.s_q);
+        // the live keys of a query are its first ones: `seen` of the block's for the first query, one more for each other
+        const int seen = a.causal ? (int)min(max(q0 + w.start - k0 + 1, (int64_t)-8), (int64_t)8) : 8;
+        if (seen + 3 <= 0) continue;
+        if (narrow) {
+            for (int i = 0; i < nq; ++i)
+                for (int j = 0; j < min(nk, seen + i); ++j)
+                    store_one<DT>(out, out0 + (q0 + i) * a.o_q + j, load_one<DT>(scores, in0 + (q0 + i) * a.s_q + j) + bias[8 * (ct + RG * tl.steps - 1 - block) + 7 + j - half - i]);
+            continue;
         }
+        float c[12];                                   // c[3 + j - i]: the bias of key j and query i of these four
+        const float4* cp = reinterpret_cast<const float4*>(bias + 8 * (ct + RG * tl.steps - 1 - block) + 4 - half);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < 3; ++i) { const float4 f = cp[i]; c[4 * i] = f.x; c[4 * i + 1] = f.y; c[4 * i + 2] = f.z; c[4 * i + 3] = f.w; }
+        Raw8<DT> r[4];
+        const int64_t at = in0 + q0 * a.s_q;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < nq) r[i] = load_raw8<DT>(scores, at + i * a.s_q);
+        const int64_t to = out0 + q0 * a.o_q;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
             if (i >= nq) break;
             float v[8];
-            if (narrow) {
-                load_first<DT>(scores, in0 + (q0 + i) * a.s_q, nk, v);
-            } else {
-                widen8<DT>(r[i], v);
-                if (over & 4)
+            widen8<DT>(r[i], v);
+            if (over) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] = last ? v[j + 4] : v[j];
-                if (over & 2)
+                for (int j = 0; j < 4; ++j) v[j] = last && (over & 4) ? v[j + 4] : v[j];
 #pragma unroll
-                    for (int j = 0; j < 6; ++j) v[j] = last ? v[j + 2] : v[j];
-                if (over & 1)
+                for (int j = 0; j < 6; ++j) v[j] = last && (over & 2) ? v[j + 2] : v[j];
 #pragma unroll
-                    for (int j = 0; j < 7; ++j) v[j] = last ? v[j + 1] : v[j];
+                for (int j = 0; j < 7; ++j) v[j] = last && (over & 1) ? v[j + 1] : v[j];
             }
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] += c[7 + j - i];
-            // the live keys of a query are its first ones
-            const int n = a.causal ? (int)min((int64_t)nk, max((int64_t)0, q0 + i + w.start - k0 + 1)) : nk;
-            const int64_t to = out0 + (q0 + i) * a.o_q;
-            if (n == 8) store8<DT>(out, to, v);
-            else        store_first<DT>(out, to, n, v);
+            for (int j = 0; j < 8; ++j) v[j] += c[3 + j - i];
+            const int n = min(nk, seen + i);
+            if (n >= 8) store8<DT>(out, to + i * a.o_q, v);
+            else        store_first<DT>(out, to + i * a.o_q, max(n, 0), f32x8{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]});
         }
     }
 }
@@ -132,6 +142,7 @@ constexpr int kMaxSlots = kThreads * 8 + 8 * (kThreads / 8);
 template <int DT>
 __global__ __launch_bounds__(kThreads, 3) void k_posbias_walk(PosbiasArgs a, const void* __restrict__ dS, Walk wk, double* __restrict__ partial, float* __restrict__ rows) {
     __shared__ double val[kMaxSlots];                  // [groups][8 LC + 8]: sums of the groups' diagonals
+    __shared__ double slot[kMaxSlots];                 // sums of the workgroup's diagonals
     __shared__ short bkt[kMaxSlots];                   // and their buckets
     const int tid = threadIdx.x, LC = 1 << wk.lc, G = kThreads >> wk.lc, P = 8 * LC + 8;
     const int li = tid & (LC - 1), g = tid >> wk.lc;
@@ -226,24 +237,15 @@ __global__ __launch_bounds__(kThreads, 3) void k_posbias_walk(PosbiasArgs a, con
     // the pieces of a band are added: a slot per diagonal of each band that this workgroup has a piece of
     const int t0 = wg * G, first = t0 / wk.segs, slots = (min(wk.bands - 1, (t0 + G - 1) / wk.segs) - first + 1) * P;
     __syncthreads();
-    double sum[kMaxSlots / kThreads];
-#pragma unroll
-    for (int i = 0; i < kMaxSlots / kThreads; ++i) {
-        const int s = tid + i * kThreads, bd = first + s / P, x = s % P;
+    for (int s = tid; s < slots; s += kThreads) {
+        const int bd = first + s / P, x = s - (bd - first) * P, end = min((bd + 1) * wk.segs - t0, G);
         double v = 0.0;
-        if (s < slots) {
-            const int end = min((bd + 1) * wk.segs - t0, G);
-            for (int t = max(bd * wk.segs - t0, 0); t < end; ++t) v += val[t * P + x];
-            const int64_t distance = (int64_t)8 * (wk.m_first + bd * LC) + x - 7 - w.start;
-            const int j = a.causal && distance > 0 ? -1 : bucket_of(a, distance);
-            bkt[s] = (short)(j >= 0 && j < a.n_buckets ? j : -1);
-        }
-        sum[i] = v;
+        for (int t = max(bd * wk.segs - t0, 0); t < end; ++t) v += val[t * P + x];
+        slot[s] = v;
+        const int64_t distance = (int64_t)8 * (wk.m_first + bd * LC) + x - 7 - w.start;
+        const int j = a.causal && distance > 0 ? -1 : bucket_of(a, distance);
+        bkt[s] = (short)(j >= 0 && j < a.n_buckets ? j : -1);
     }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kMaxSlots / kThreads; ++i)
-        if (tid + i * kThreads < slots) val[tid + i * kThreads] = sum[i];
     __syncthreads();
     // 2^ul threads for a bucket look through all slots
     int ul = 6;
@@ -257,11 +259,11 @@ __global__ __launch_bounds__(kThreads, 3) void k_posbias_walk(PosbiasArgs a, con
             double v[8];
             int c[8];
 #pragma unroll
-            for (int y = 0; y < 8; ++y) { v[y] = val[k + (y << ul)]; c[y] = bkt[k + (y << ul)]; }
+            for (int y = 0; y < 8; ++y) { v[y] = slot[k + (y << ul)]; c[y] = bkt[k + (y << ul)]; }
 #pragma unroll
             for (int y = 0; y < 8; ++y) s += c[y] == j ? v[y] : 0.0;
         }
-        for (; k < slots; k += 1 << ul) s += bkt[k] == j ? val[k] : 0.0;
+        for (; k < slots; k += 1 << ul) s += bkt[k] == j ? slot[k] : 0.0;
         for (int off = 1; off < 1 << ul; off <<= 1) s += __shfl_xor(s, off, kWave);
         if (u == 0 && j < a.n_buckets) {
             if (wk.wgs == 1) rows[((int64_t)b * a.n_buckets + j) * a.H + h] = (float)s;
