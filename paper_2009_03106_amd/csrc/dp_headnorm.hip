@@ -22,41 +22,87 @@ struct Rows {
 };
 
 // The pairs of a row: V next to each other at a time, N times for a lane.
-//   V == 1: pair p of lane l is l + i L; its numbers are columns a and b (b beyond D: none)
-//   V == 8: pair 8 l and the seven behind; D and rot are multiples of 16
-// PAIRS (V == 8): neighbours turn together, so the 16 columns are one piece.
+//   V == 1: pair l + i L for lane l, any D and rot
+//   V == 8: pairs 8 l to 8 l + 7, D and rot multiples of 16: two pieces of eight numbers (16 bytes; float32: 32) for a lane
+// PAIRS (V == 8): neighbours turn together, the pieces are next to each other; else they are half of `rot` apart, and next to
+// each other behind the numbers that turn.
 __device__ __forceinline__ int2 columns(const HeadnormArgs& a, int p) {
     if (a.pairs) return make_int2(2 * p, 2 * p + 1);
     const int half = a.rot / 2;
     return p < half ? make_int2(p, p + half) : make_int2(2 * p, 2 * p + 1);
 }
+template <bool PAIRS> __device__ __forceinline__ int2 pieces(const HeadnormArgs& a, int l) {
+    const int half = a.rot / 2;
+    return PAIRS || 8 * l >= half ? make_int2(16 * l, 16 * l + 8) : make_int2(8 * l, 8 * l + half);
+}
 
 template <int DT, int V, int N, bool PAIRS> struct Row {
-    float lo[V * N], hi[V * N];            // the pairs' numbers: (lo[i], hi[i]) turn together (PAIRS: neighbours within lo and within hi)
+    float lo[V * N], hi[V * N];            // (lo[i], hi[i]) turn together; PAIRS: neighbours within lo, and within hi
 
     __device__ __forceinline__ void load(const HeadnormArgs& a, const void* p, int64_t at, int l, int L, bool live) {
-        static_assert(V == 1, "one pair at a time");
+        if constexpr (V == 8) {
+            const int2 c = pieces<PAIRS>(a, l);
+            Raw8<DT> x{}, y{};
+            if (live && 16 * l < a.D) {
+                x = load_raw8<DT>(p, at + c.x);
+                y = load_raw8<DT>(p, at + c.y);
+            }
+            widen8<DT>(x, lo);
+            widen8<DT>(y, hi);
+        } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int2 c = columns(a, l + i * L);
-            lo[i] = live && c.x < a.D ? load_one<DT>(p, at + c.x) : 0.f;
-            hi[i] = live && c.y < a.D ? load_one<DT>(p, at + c.y) : 0.f;
+            for (int i = 0; i < N; ++i) {
+                const int2 c = columns(a, l + i * L);
+                lo[i] = live && c.x < a.D ? load_one<DT>(p, at + c.x) : 0.f;
+                hi[i] = live && c.y < a.D ? load_one<DT>(p, at + c.y) : 0.f;
+            }
         }
     }
     __device__ __forceinline__ void store(const HeadnormArgs& a, void* p, int64_t at, int l, int L) const {
+        if constexpr (V == 8) {
+            const int2 c = pieces<PAIRS>(a, l);
+            if (16 * l < a.D) {
+                store8<DT>(p, at + c.x, lo);
+                store8<DT>(p, at + c.y, hi);
+            }
+        } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int2 c = columns(a, l + i * L);
-            if (c.x < a.D) store_one<DT>(p, at + c.x, lo[i]);
-            if (c.y < a.D) store_one<DT>(p, at + c.y, hi[i]);
+            for (int i = 0; i < N; ++i) {
+                const int2 c = columns(a, l + i * L);
+                if (c.x < a.D) store_one<DT>(p, at + c.x, lo[i]);
+                if (c.y < a.D) store_one<DT>(p, at + c.y, hi[i]);
+            }
         }
     }
     __device__ __forceinline__ void to_lds(const HeadnormArgs& a, float* row, int l, int L) const {
+        if constexpr (V == 8) {
+            const int2 c = pieces<PAIRS>(a, l);
+            if (16 * l < a.D) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int2 c = columns(a, l + i * L);
-            if (c.x < a.D) row[c.x] = lo[i];
-            if (c.y < a.D) row[c.y] = hi[i];
+                for (int i = 0; i < 8; ++i) { row[c.x + i] = lo[i]; row[c.y + i] = hi[i]; }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int2 c = columns(a, l + i * L);
+                if (c.x < a.D) row[c.x] = lo[i];
+                if (c.y < a.D) row[c.y] = hi[i];
+            }
+        }
+    }
+    // the pairs, by the angles whose sines and cosines these are (sign -1: back)
+    __device__ __forceinline__ void rotate(const float (&s)[V * N], const float (&c)[V * N], float sign) {
+        const auto one = [&](float& x, float& y, int k) {
+            const float sk = sign * s[k], t = x * c[k] - y * sk;
+            y = x * sk + y * c[k];
+            x = t;
+        };
+        if constexpr (PAIRS) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { one(lo[2 * i], lo[2 * i + 1], i); one(hi[2 * i], hi[2 * i + 1], 4 + i); }
+        } else {
+#pragma unroll
+            for (int i = 0; i < V * N; ++i) one(lo[i], hi[i], i);
         }
     }
 };
@@ -124,26 +170,30 @@ __global__ __launch_bounds__(kThreads) void k_headnorm(HeadnormArgs a, Rows w) {
         const Token k = token_of(a, n0 + g / w.hw);
         Turn<V, N> turn;
         turn.of(a, k.position, l, w.L, k.live);
-        for (int it = it0; it < it1; ++it) {
-            const int which = it >= w.its0;
+#pragma unroll 1
+        for (int which = it0 >= w.its0; which <= (it1 > w.its0); ++which) {
             const HeadsArgs& hd = a.heads[which];
-            const int h = (which ? it - w.its0 : it) * w.hw + (g & (w.hw - 1));
-            const bool live = k.live && h < hd.H;
-            Row<DT, V, N, PAIRS> x;
+            const int first = which ? w.its0 : 0, from = max(it0, first), to = which ? it1 : min(it1, w.its0);
             Row<0, V, N, PAIRS> gain;
-            x.load(a, hd.x, k.b * hd.x_b + k.t * hd.x_t + h * hd.x_h, l, w.L, live);
             gain.load(a, hd.gain, 0, l, w.L, true);
-            float sq = 0.f;
+            const int64_t in = k.b * hd.x_b + k.t * hd.x_t, out = k.b * hd.o_b + k.t * hd.o_t;
+            for (int it = from; it < to; ++it) {
+                const int h = (it - first) * w.hw + (g & (w.hw - 1));
+                const bool live = k.live && h < hd.H;
+                Row<DT, V, N, PAIRS> x;
+                x.load(a, hd.x, in + h * hd.x_h, l, w.L, live);
+                float sq = 0.f;
 #pragma unroll
-            for (int i = 0; i < V * N; ++i) sq += x.lo[i] * x.lo[i] + x.hi[i] * x.hi[i];
-            const float r = 1.0f / sqrtf(row_sum(sq, w.L) * mean + a.eps);
+                for (int i = 0; i < V * N; ++i) sq += x.lo[i] * x.lo[i] + x.hi[i] * x.hi[i];
+                const float r = 1.0f / sqrtf(row_sum(sq, w.L) * mean + a.eps);
 #pragma unroll
-            for (int i = 0; i < V * N; ++i) {
-                const float lo = x.lo[i] * r * gain.lo[i], hi = x.hi[i] * r * gain.hi[i];
-                x.lo[i] = lo * turn.c[i] - hi * turn.s[i];
-                x.hi[i] = lo * turn.s[i] + hi * turn.c[i];
+                for (int i = 0; i < V * N; ++i) {
+                    x.lo[i] *= r * gain.lo[i];
+                    x.hi[i] *= r * gain.hi[i];
+                }
+                x.rotate(turn.s, turn.c, 1.0f);
+                if (live) x.store(a, hd.out, out + h * hd.o_h, l, w.L);
             }
-            if (live) x.store(a, hd.out, k.b * hd.o_b + k.t * hd.o_t + h * hd.o_h, l, w.L);
         }
     }
 }
@@ -176,16 +226,16 @@ __global__ __launch_bounds__(kThreads) void k_headnorm_back(HeadnormArgs a, Rows
 #pragma unroll
             for (int i = 0; i < V * N; ++i) sq += x.lo[i] * x.lo[i] + x.hi[i] * x.hi[i];
             const float r = 1.0f / sqrtf(row_sum(sq, w.L) * mean + a.eps);
+            u.rotate(turn.s, turn.c, -1.0f);
             float dot = 0.f;
 #pragma unroll
             for (int i = 0; i < V * N; ++i) {
-                const float lo = u.lo[i] * turn.c[i] + u.hi[i] * turn.s[i], hi = u.hi[i] * turn.c[i] - u.lo[i] * turn.s[i];
                 x.lo[i] *= r;
                 x.hi[i] *= r;
-                gg.lo[i] += lo * x.lo[i];
-                gg.hi[i] += hi * x.hi[i];
-                u.lo[i] = lo * gain.lo[i];
-                u.hi[i] = hi * gain.hi[i];
+                gg.lo[i] += u.lo[i] * x.lo[i];
+                gg.hi[i] += u.hi[i] * x.hi[i];
+                u.lo[i] *= gain.lo[i];
+                u.hi[i] *= gain.hi[i];
                 dot += u.lo[i] * x.lo[i] + u.hi[i] * x.hi[i];
             }
             dot = row_sum(dot, w.L) * mean;
@@ -243,7 +293,10 @@ int pow2_up(int n) {
 
 // pairs of a lane and lanes of a row
 struct Shape { int V, N, L; };
+// (16-byte pieces where D and rot are multiples of 16; numbers one by one took 500 us instead of the pieces' for
+// 4 x 8192 tokens of 32 + 8 heads of 128 bf16)
 Shape shape_of(const HeadnormArgs& a) {
+    if (a.D % 16 == 0 && a.rot % 16 == 0) return Shape{8, 1, pow2_up(a.D / 16)};
     const int pairs = (a.D + 1) / 2, L = std::min(kWave, pow2_up(pairs));
     return Shape{1, pow2_up((pairs + L - 1) / L), L};
 }
@@ -281,13 +334,17 @@ template <int DT, int V, int N, bool PAIRS> void backward_as(const HeadnormArgs&
 }
 
 template <int DT> void forward(const HeadnormArgs& a, const Shape& s, const Rows& w, int grid, hipStream_t st) {
-    if (s.N == 1)      forward_as<DT, 1, 1, false>(a, w, grid, st);
+    if (s.V == 8 && a.pairs) forward_as<DT, 8, 1, true>(a, w, grid, st);
+    else if (s.V == 8) forward_as<DT, 8, 1, false>(a, w, grid, st);
+    else if (s.N == 1) forward_as<DT, 1, 1, false>(a, w, grid, st);
     else if (s.N == 2) forward_as<DT, 1, 2, false>(a, w, grid, st);
     else if (s.N == 4) forward_as<DT, 1, 4, false>(a, w, grid, st);
     else               forward_as<DT, 1, 8, false>(a, w, grid, st);
 }
 template <int DT> void backward(const HeadnormArgs& a, const Shape& s, const Rows& w, int tokens, int chunks, float* partial, hipStream_t st) {
-    if (s.N == 1)      backward_as<DT, 1, 1, false>(a, w, tokens, chunks, partial, st);
+    if (s.V == 8 && a.pairs) backward_as<DT, 8, 1, true>(a, w, tokens, chunks, partial, st);
+    else if (s.V == 8) backward_as<DT, 8, 1, false>(a, w, tokens, chunks, partial, st);
+    else if (s.N == 1) backward_as<DT, 1, 1, false>(a, w, tokens, chunks, partial, st);
     else if (s.N == 2) backward_as<DT, 1, 2, false>(a, w, tokens, chunks, partial, st);
     else if (s.N == 4) backward_as<DT, 1, 4, false>(a, w, tokens, chunks, partial, st);
     else               backward_as<DT, 1, 8, false>(a, w, tokens, chunks, partial, st);
