@@ -36,19 +36,20 @@ template <bool PAIRS> __device__ __forceinline__ int2 pieces(const HeadnormArgs&
     return PAIRS || 8 * l >= half ? make_int2(16 * l, 16 * l + 8) : make_int2(8 * l, 8 * l + half);
 }
 
-template <int DT, int V, int N, bool PAIRS> struct Row {
-    float lo[V * N], hi[V * N];            // (lo[i], hi[i]) turn together; PAIRS: neighbours within lo, and within hi
-
+// a lane's numbers of a row on their way: as they are in memory, zeros where there are none
+template <int DT, int V, int N, bool PAIRS> struct Fetched {
+    static constexpr int kOnes = V == 8 ? 1 : N;
+    Raw8<DT> x, y;
+    float lo[kOnes], hi[kOnes];
     __device__ __forceinline__ void load(const HeadnormArgs& a, const void* p, int64_t at, int l, int L, bool live) {
         if constexpr (V == 8) {
             const int2 c = pieces<PAIRS>(a, l);
-            Raw8<DT> x{}, y{};
+            x = Raw8<DT>{};
+            y = Raw8<DT>{};
             if (live && 16 * l < a.D) {
                 x = load_raw8<DT>(p, at + c.x);
                 y = load_raw8<DT>(p, at + c.y);
             }
-            widen8<DT>(x, lo);
-            widen8<DT>(y, hi);
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -57,6 +58,25 @@ template <int DT, int V, int N, bool PAIRS> struct Row {
                 hi[i] = live && c.y < a.D ? load_one<DT>(p, at + c.y) : 0.f;
             }
         }
+    }
+};
+
+template <int DT, int V, int N, bool PAIRS> struct Row {
+    float lo[V * N], hi[V * N];            // (lo[i], hi[i]) turn together; PAIRS: neighbours within lo, and within hi
+
+    __device__ __forceinline__ void take(const Fetched<DT, V, N, PAIRS>& f) {
+        if constexpr (V == 8) {
+            widen8<DT>(f.x, lo);
+            widen8<DT>(f.y, hi);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) { lo[i] = f.lo[i]; hi[i] = f.hi[i]; }
+        }
+    }
+    __device__ __forceinline__ void load(const HeadnormArgs& a, const void* p, int64_t at, int l, int L, bool live) {
+        Fetched<DT, V, N, PAIRS> f;
+        f.load(a, p, at, l, L, live);
+        take(f);
     }
     __device__ __forceinline__ void store(const HeadnormArgs& a, void* p, int64_t at, int l, int L) const {
         if constexpr (V == 8) {
@@ -198,91 +218,156 @@ __global__ __launch_bounds__(kThreads) void k_headnorm(HeadnormArgs a, Rows w) {
     }
 }
 
-// Backward.  A workgroup has `tokens` of an example's tokens; its sums of the gains' gradients go to partial[b][chunk][descriptor][D].
+// Backward.  A workgroup has some tokens of an example and all of one descriptor's heads: the gains' gradients of a lane's columns
+// stay in its registers.  `split` of its waves share a token's heads.  The next row's numbers are on their way while one is worked
+// on.  The sums go to partial[example][chunk][D] of the descriptor.
+struct Back {
+    Rows w;
+    int tokens, chunks;        // of a workgroup, of an example
+    float* partial;
+};
+struct BackPlan { Back of[2]; int first; };            // workgroups from `first` on have the second descriptor's heads
+
 template <int DT, int V, int N, bool PAIRS>
-__global__ __launch_bounds__(kThreads) void k_headnorm_back(HeadnormArgs a, Rows w, int tokens, int chunks, float* __restrict__ partial) {
-    extern __shared__ float sums[];                    // [waves][descriptors][D]
-    constexpr int kWaves = kThreads / kWave;
-    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane & (w.L - 1), g = lane / w.L;
-    const int b = blockIdx.x / chunks, chunk = blockIdx.x - b * chunks;
-    const int t0 = chunk * tokens, t1 = min(t0 + tokens, a.T);
+__global__ __launch_bounds__(kThreads) void k_headnorm_back(HeadnormArgs a, BackPlan plan) {
+    __shared__ float sums[kThreads / kWave][kMaxHeadDim];
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int which = (int)blockIdx.x >= plan.first;
+    const Back& bk = plan.of[which];
+    const Rows& w = bk.w;
+    const HeadsArgs& hd = a.heads[which];
+    const int l = lane & (w.L - 1), g = lane / w.L, wg = blockIdx.x - (which ? plan.first : 0);
+    const int b = wg / bk.chunks, chunk = wg - b * bk.chunks;
+    const int part = wave % w.split, it0 = w.its * part / w.split, it1 = w.its * (part + 1) / w.split;
+    const int64_t t0 = (int64_t)chunk * bk.tokens;
+    const int end = (int)min(t0 + bk.tokens, (int64_t)(a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T));
+    const int step = kThreads / kWave / w.split * w.tw;
     const float mean = 1.0f / a.D;
-    Row<0, V, N, PAIRS> acc[2] = {};
-    for (int base = t0 + wave * w.tw; base < t1; base += kWaves * w.tw) {
-        const int t = base + g / w.hw;
-        Token k = token_of(a, (int64_t)b * a.T + min(t, t1 - 1));
-        k.live = k.live && t < t1;
-        Turn<V, N> turn;
-        turn.of(a, k.position, l, w.L, k.live);
-        auto step = [&](const HeadsArgs& hd, int it, Row<0, V, N, PAIRS>& gg) {
-            const int h = it * w.hw + (g & (w.hw - 1));
-            const bool live = k.live && h < hd.H;
-            Row<DT, V, N, PAIRS> x, u;
-            Row<0, V, N, PAIRS> gain;
-            x.load(a, hd.x, k.b * hd.x_b + k.t * hd.x_t + h * hd.x_h, l, w.L, live);
-            u.load(a, hd.dy, k.b * hd.dy_b + k.t * hd.dy_t + h * hd.dy_h, l, w.L, live);
-            gain.load(a, hd.gain, 0, l, w.L, true);
-            float sq = 0.f;
+    Row<0, V, N, PAIRS> acc = {}, gain;
+    gain.load(a, hd.gain, 0, l, w.L, true);
+    Turn<V, N> turn;
+    Fetched<DT, V, N, PAIRS> fx, fu;
+    const int64_t x0 = b * hd.x_b, u0 = b * hd.dy_b, o0 = b * hd.o_b;
+    const int hl = g & (w.hw - 1);
+    int64_t n = t0 + wave / w.split * w.tw;            // the first of the wave's tokens; t the lane's
+    int it = it0;
+    const auto fetch = [&](int64_t n, int it) {
+        const int64_t t = n + g / w.hw;
+        const int h = it * w.hw + hl;
+        const bool live = t < end && h < hd.H;
+        fx.load(a, hd.x, x0 + t * hd.x_t + h * hd.x_h, l, w.L, live);
+        fu.load(a, hd.dy, u0 + t * hd.dy_t + h * hd.dy_h, l, w.L, live);
+    };
+    if (it0 < it1 && n < end) fetch(n, it);
+    while (it0 < it1 && n < end) {
+        const int64_t t = n + g / w.hw;
+        if (it == it0) {
+            const bool live = t < end;
+            const int position = !live ? 0 : a.positions ? a.positions[b * a.positions_b + t] : (int)t;
+            turn.of(a, position, l, w.L, live);
+        }
+        Row<DT, V, N, PAIRS> x, u;
+        x.take(fx);
+        u.take(fu);
+        const int h = it * w.hw + hl;
+        const bool live = t < end && h < hd.H;
+        if (++it == it1) { it = it0; n += step; }
+        if (n < end) fetch(n, it);
+        float sq = 0.f;
 #pragma unroll
-            for (int i = 0; i < V * N; ++i) sq += x.lo[i] * x.lo[i] + x.hi[i] * x.hi[i];
-            const float r = 1.0f / sqrtf(row_sum(sq, w.L) * mean + a.eps);
-            u.rotate(turn.s, turn.c, -1.0f);
-            float dot = 0.f;
+        for (int i = 0; i < V * N; ++i) sq += x.lo[i] * x.lo[i] + x.hi[i] * x.hi[i];
+        const float r = 1.0f / sqrtf(row_sum(sq, w.L) * mean + a.eps);
+        u.rotate(turn.s, turn.c, -1.0f);
+        float dot = 0.f;
 #pragma unroll
-            for (int i = 0; i < V * N; ++i) {
-                x.lo[i] *= r;
-                x.hi[i] *= r;
-                gg.lo[i] += u.lo[i] * x.lo[i];
-                gg.hi[i] += u.hi[i] * x.hi[i];
-                u.lo[i] *= gain.lo[i];
-                u.hi[i] *= gain.hi[i];
-                dot += u.lo[i] * x.lo[i] + u.hi[i] * x.hi[i];
-            }
-            dot = row_sum(dot, w.L) * mean;
+        for (int i = 0; i < V * N; ++i) {
+            x.lo[i] *= r;
+            x.hi[i] *= r;
+            acc.lo[i] += u.lo[i] * x.lo[i];
+            acc.hi[i] += u.hi[i] * x.hi[i];
+            u.lo[i] *= gain.lo[i];
+            u.hi[i] *= gain.hi[i];
+            dot += u.lo[i] * x.lo[i] + u.hi[i] * x.hi[i];
+        }
+        dot = row_sum(dot, w.L) * mean;
 #pragma unroll
-            for (int i = 0; i < V * N; ++i) {
-                x.lo[i] = r * (u.lo[i] - x.lo[i] * dot);
-                x.hi[i] = r * (u.hi[i] - x.hi[i] * dot);
-            }
-            if (live) x.store(a, hd.out, k.b * hd.o_b + k.t * hd.o_t + h * hd.o_h, l, w.L);
-        };
-        for (int it = 0; it < w.its0; ++it) step(a.heads[0], it, acc[0]);
-        for (int it = w.its0; it < w.its; ++it) step(a.heads[1], it - w.its0, acc[1]);
+        for (int i = 0; i < V * N; ++i) {
+            x.lo[i] = r * (u.lo[i] - x.lo[i] * dot);
+            x.hi[i] = r * (u.hi[i] - x.hi[i] * dot);
+        }
+        if (live) x.store(a, hd.out, o0 + t * hd.o_t + h * hd.o_h, l, w.L);
     }
     // the rows of a wave, then the waves, in a fixed order
 #pragma unroll
-    for (int which = 0; which < 2; ++which) {
-        if (which >= a.n_heads) break;
-#pragma unroll
-        for (int i = 0; i < V * N; ++i)
-            for (int off = w.L; off < kWave; off <<= 1) {
-                acc[which].lo[i] += __shfl_xor(acc[which].lo[i], off, kWave);
-                acc[which].hi[i] += __shfl_xor(acc[which].hi[i], off, kWave);
-            }
-        if (g == 0) acc[which].to_lds(a, sums + (wave * a.n_heads + which) * a.D, l, w.L);
-    }
+    for (int i = 0; i < V * N; ++i)
+        for (int off = w.L; off < kWave; off <<= 1) {
+            acc.lo[i] += __shfl_xor(acc.lo[i], off, kWave);
+            acc.hi[i] += __shfl_xor(acc.hi[i], off, kWave);
+        }
+    if (g == 0) acc.to_lds(a, sums[wave], l, w.L);
     __syncthreads();
-    const int n = a.n_heads * a.D;
-    for (int j = threadIdx.x; j < n; j += kThreads)
-        partial[(int64_t)blockIdx.x * n + j] = (sums[j] + sums[n + j]) + (sums[2 * n + j] + sums[3 * n + j]);
+    for (int j = threadIdx.x; j < a.D; j += kThreads)
+        bk.partial[(int64_t)wg * a.D + j] = (sums[0][j] + sums[1][j]) + (sums[2][j] + sums[3][j]);
 }
 
-// A workgroup per example: the chunks' sums, and the squared norm of the rows.
-__global__ __launch_bounds__(kThreads) void k_headnorm_fold(HeadnormArgs a, int chunks, const float* __restrict__ partial, int accumulate, float* __restrict__ sqnorm) {
-    __shared__ double red[4];
-    const int b = blockIdx.x, n = a.n_heads * a.D;
-    const float* p = partial + (int64_t)b * chunks * n;
+// A workgroup per example: the chunks' sums, by groups of threads for as many columns (W next to each other for a thread), and the
+// squared norm of the rows.
+constexpr int kFoldThreads = 1024;
+template <int W>
+__global__ __launch_bounds__(kFoldThreads) void k_headnorm_fold(HeadnormArgs a, BackPlan plan, int accumulate, float* __restrict__ sqnorm) {
+    __shared__ double part[kFoldThreads][W];
+    __shared__ double red[kFoldThreads / kWave];
+    const int b = blockIdx.x, columns = a.D / W;
+    int ct = 1;                                        // threads along the columns, a power of two
+    while (ct < columns && ct < kFoldThreads) ct *= 2;
+    const int groups = kFoldThreads / ct, c = threadIdx.x & (ct - 1), g = threadIdx.x / ct;
     double sq = 0.0;
-    for (int j = threadIdx.x; j < n; j += kThreads) {
-        double s = 0.0;
-        for (int c = 0; c < chunks; ++c) s += p[(int64_t)c * n + j];
-        const float v = (float)s;
-        const int which = j >= a.D;
-        a.heads[which].gain_rows[(int64_t)b * a.D + (which ? j - a.D : j)] = v;
-        sq += (double)v * v;
+    for (int which = 0; which < a.n_heads; ++which) {
+        const Back& bk = plan.of[which];
+        const float* p = bk.partial + (int64_t)b * bk.chunks * a.D + c * W;
+        double s[W];
+#pragma unroll
+        for (int v = 0; v < W; ++v) s[v] = 0.0;
+        if (c < columns) {
+            int k = g;
+            for (; k + 3 * groups < bk.chunks; k += 4 * groups) {
+                float f[4][W];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int v = 0; v < W; ++v) f[i][v] = p[(int64_t)(k + i * groups) * a.D + v];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int v = 0; v < W; ++v) s[v] += f[i][v];
+            }
+            for (; k < bk.chunks; k += groups)
+#pragma unroll
+                for (int v = 0; v < W; ++v) s[v] += p[(int64_t)k * a.D + v];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int v = 0; v < W; ++v) part[threadIdx.x][v] = s[v];
+        __syncthreads();
+        if (g == 0 && c < columns) {
+            for (int k = 1; k < groups; ++k)
+#pragma unroll
+                for (int v = 0; v < W; ++v) s[v] += part[k * ct + c][v];
+#pragma unroll
+            for (int v = 0; v < W; ++v) {
+                const float f = (float)s[v];
+                a.heads[which].gain_rows[(int64_t)b * a.D + c * W + v] = f;
+                sq += (double)f * f;
+            }
+        }
     }
-    sq = block_sum_256_f64(sq, red);
-    if (threadIdx.x == 0) sqnorm[b] = (float)(accumulate ? sqnorm[b] + sq : sq);
+    sq = wave_sum_f64(sq);
+    if ((threadIdx.x & (kWave - 1)) == 0) red[threadIdx.x >> 6] = sq;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+#pragma unroll
+    for (int k = 1; k < kFoldThreads / kWave; ++k) sq += red[k];
+    sqnorm[b] = (float)(accumulate ? sqnorm[b] + sq : sq);
 }
 
 int pow2_up(int n) {
@@ -303,8 +388,8 @@ Shape shape_of(const HeadnormArgs& a) {
 
 // Heads and tokens of a wave: as many heads (which lie next to each other) as leave at most a tenth of the rows idle, else the
 // number with the fewest idle ones.
-Rows rows_of(const HeadnormArgs& a, int L) {
-    const int W = kWave / L, H0 = a.heads[0].H, H1 = a.heads[1].H;
+Rows rows_of(int H0, int H1, int L) {
+    const int W = kWave / L;
     Rows w{};
     w.L = L;
     int64_t least = INT64_MAX;
@@ -320,17 +405,42 @@ Rows rows_of(const HeadnormArgs& a, int L) {
     return w;
 }
 
-// Chunks of an example's tokens in the backward pass: about eight workgroups for each of the 256 compute units, of at least 16 tokens.
-int back_chunks(int B, int T) {
-    return (int)std::max<int64_t>(1, std::min<int64_t>({512, (2048 + B - 1) / (int64_t)B, (T + 15) / 16}));
+// The most chunks that an example's tokens are cut into in the backward pass: 1536 workgroups in all (twice what the 256 compute
+// units have registers for at a time), and no more than the fold adds up in a few microseconds.
+constexpr int kBackGroups = 1536, kBackChunks = 512;
+int most_chunks(int B, int T) { return std::max(1, std::min({kBackChunks, T, kBackGroups / B})); }
+
+// Descriptors with more heads get shorter chunks, so that all workgroups have about the same number of rows.  Where waves are few,
+// two or four of a workgroup share a token's heads.
+BackPlan plan_back(const HeadnormArgs& a, int L, float* partial) {
+    BackPlan p{};
+    const int waves = kThreads / kWave, most = most_chunks(a.B, a.T);
+    int64_t steps = 0;                                  // of all waves together
+    for (int i = 0; i < a.n_heads; ++i) {
+        Rows& w = p.of[i].w;
+        w = rows_of(a.heads[i].H, 0, L);
+        steps += (int64_t)a.B * ceil_div(a.T, w.tw) * w.its;
+    }
+    const int64_t per_wave = std::max<int64_t>(1, steps / (kBackGroups * waves));
+    for (int i = 0; i < a.n_heads; ++i) {
+        Back& k = p.of[i];
+        while (k.w.split < waves && k.w.split * 2 <= k.w.its && k.w.its / k.w.split > per_wave) k.w.split *= 2;
+        const int granule = waves / k.w.split * k.w.tw; // tokens that a workgroup has at a time
+        const int64_t rounds = std::max<int64_t>(1, per_wave * k.w.split / std::max(1, k.w.its));
+        k.tokens = (int)std::min<int64_t>(a.T, granule * std::max<int64_t>(rounds, ceil_div(ceil_div(a.T, granule), most)));
+        k.chunks = ceil_div(a.T, k.tokens);
+        k.partial = partial;
+        partial += (int64_t)a.B * most * a.D;
+    }
+    p.first = a.B * p.of[0].chunks;
+    return p;
 }
 
 template <int DT, int V, int N, bool PAIRS> void forward_as(const HeadnormArgs& a, const Rows& w, int grid, hipStream_t st) {
     k_headnorm<DT, V, N, PAIRS><<<grid, kThreads, 0, st>>>(a, w);
 }
-template <int DT, int V, int N, bool PAIRS> void backward_as(const HeadnormArgs& a, const Rows& w, int tokens, int chunks, float* partial, hipStream_t st) {
-    const size_t lds = (size_t)(kThreads / kWave) * a.n_heads * a.D * sizeof(float);
-    k_headnorm_back<DT, V, N, PAIRS><<<a.B * chunks, kThreads, lds, st>>>(a, w, tokens, chunks, partial);
+template <int DT, int V, int N, bool PAIRS> void backward_as(const HeadnormArgs& a, const BackPlan& p, hipStream_t st) {
+    k_headnorm_back<DT, V, N, PAIRS><<<a.B * (p.of[0].chunks + p.of[1].chunks), kThreads, 0, st>>>(a, p);
 }
 
 template <int DT> void forward(const HeadnormArgs& a, const Shape& s, const Rows& w, int grid, hipStream_t st) {
@@ -341,13 +451,13 @@ template <int DT> void forward(const HeadnormArgs& a, const Shape& s, const Rows
     else if (s.N == 4) forward_as<DT, 1, 4, false>(a, w, grid, st);
     else               forward_as<DT, 1, 8, false>(a, w, grid, st);
 }
-template <int DT> void backward(const HeadnormArgs& a, const Shape& s, const Rows& w, int tokens, int chunks, float* partial, hipStream_t st) {
-    if (s.V == 8 && a.pairs) backward_as<DT, 8, 1, true>(a, w, tokens, chunks, partial, st);
-    else if (s.V == 8) backward_as<DT, 8, 1, false>(a, w, tokens, chunks, partial, st);
-    else if (s.N == 1) backward_as<DT, 1, 1, false>(a, w, tokens, chunks, partial, st);
-    else if (s.N == 2) backward_as<DT, 1, 2, false>(a, w, tokens, chunks, partial, st);
-    else if (s.N == 4) backward_as<DT, 1, 4, false>(a, w, tokens, chunks, partial, st);
-    else               backward_as<DT, 1, 8, false>(a, w, tokens, chunks, partial, st);
+template <int DT> void backward(const HeadnormArgs& a, const Shape& s, const BackPlan& p, hipStream_t st) {
+    if (s.V == 8 && a.pairs) backward_as<DT, 8, 1, true>(a, p, st);
+    else if (s.V == 8) backward_as<DT, 8, 1, false>(a, p, st);
+    else if (s.N == 1) backward_as<DT, 1, 1, false>(a, p, st);
+    else if (s.N == 2) backward_as<DT, 1, 2, false>(a, p, st);
+    else if (s.N == 4) backward_as<DT, 1, 4, false>(a, p, st);
+    else               backward_as<DT, 1, 8, false>(a, p, st);
 }
 
 }  // namespace
@@ -357,11 +467,11 @@ bool headnorm_fits(int64_t B, int64_t T, int64_t H0, int64_t H1) {
     if (B > (int64_t(1) << 22) || T > most || H0 > most || H1 > most) return false;
     return B == 0 || T <= most / B;
 }
-size_t headnorm_ws_bytes(int n_heads, int B, int T, int D) { return (size_t)B * back_chunks(B, T) * n_heads * D * sizeof(float); }
+size_t headnorm_ws_bytes(int n_heads, int B, int T, int D) { return (size_t)B * most_chunks(B, T) * n_heads * D * sizeof(float); }
 
 hipError_t launch_headnorm(const HeadnormArgs& a, int dt, hipStream_t st) {
     const Shape s = shape_of(a);
-    Rows w = rows_of(a, s.L);
+    Rows w = rows_of(a.heads[0].H, a.heads[1].H, s.L);
     // a wave for every tw tokens; where that leaves the chip empty, several waves share a token's heads
     const int64_t groups = ((int64_t)a.B * a.T + w.tw - 1) / w.tw;
     w.split = (int)std::max<int64_t>(1, std::min<int64_t>(w.its, 4096 / groups));
@@ -377,15 +487,14 @@ hipError_t launch_headnorm(const HeadnormArgs& a, int dt, hipStream_t st) {
 
 hipError_t launch_headnorm_sqnorm(const HeadnormArgs& a, int dt, bool accumulate, float* sqnorm, void* ws, hipStream_t st) {
     const Shape s = shape_of(a);
-    const Rows w = rows_of(a, s.L);
-    const int chunks = back_chunks(a.B, a.T), tokens = ceil_div(a.T, chunks);
-    float* partial = static_cast<float*>(ws);
-    if (dt == 0)      backward<0>(a, s, w, tokens, chunks, partial, st);
-    else if (dt == 1) backward<1>(a, s, w, tokens, chunks, partial, st);
-    else              backward<2>(a, s, w, tokens, chunks, partial, st);
+    const BackPlan p = plan_back(a, s.L, static_cast<float*>(ws));
+    if (dt == 0)      backward<0>(a, s, p, st);
+    else if (dt == 1) backward<1>(a, s, p, st);
+    else              backward<2>(a, s, p, st);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    k_headnorm_fold<<<a.B, kThreads, 0, st>>>(a, chunks, partial, accumulate, sqnorm);
+    if (a.D % 4 == 0) k_headnorm_fold<4><<<a.B, kFoldThreads, 0, st>>>(a, p, accumulate, sqnorm);
+    else              k_headnorm_fold<1><<<a.B, kFoldThreads, 0, st>>>(a, p, accumulate, sqnorm);
     return hipGetLastError();
 }
 
