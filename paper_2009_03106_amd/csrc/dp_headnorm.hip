@@ -36,20 +36,20 @@ template <bool PAIRS> __device__ __forceinline__ int2 pieces(const HeadnormArgs&
     return PAIRS || 8 * l >= half ? make_int2(16 * l, 16 * l + 8) : make_int2(8 * l, 8 * l + half);
 }
 
-// a lane's numbers of a row on their way: as they are in memory, zeros where there are none
-template <int DT, int V, int N, bool PAIRS> struct Fetched {
-    static constexpr int kOnes = V == 8 ? 1 : N;
-    Raw8<DT> x, y;
-    float lo[kOnes], hi[kOnes];
+template <int DT, int V, int N, bool PAIRS> struct Row {
+    float lo[V * N], hi[V * N];            // (lo[i], hi[i]) turn together; PAIRS: neighbours within lo, and within hi
+
+    // zeros where there are none
     __device__ __forceinline__ void load(const HeadnormArgs& a, const void* p, int64_t at, int l, int L, bool live) {
         if constexpr (V == 8) {
             const int2 c = pieces<PAIRS>(a, l);
-            x = Raw8<DT>{};
-            y = Raw8<DT>{};
+            Raw8<DT> x{}, y{};
             if (live && 16 * l < a.D) {
                 x = load_raw8<DT>(p, at + c.x);
                 y = load_raw8<DT>(p, at + c.y);
             }
+            widen8<DT>(x, lo);
+            widen8<DT>(y, hi);
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -58,25 +58,6 @@ template <int DT, int V, int N, bool PAIRS> struct Fetched {
                 hi[i] = live && c.y < a.D ? load_one<DT>(p, at + c.y) : 0.f;
             }
         }
-    }
-};
-
-template <int DT, int V, int N, bool PAIRS> struct Row {
-    float lo[V * N], hi[V * N];            // (lo[i], hi[i]) turn together; PAIRS: neighbours within lo, and within hi
-
-    __device__ __forceinline__ void take(const Fetched<DT, V, N, PAIRS>& f) {
-        if constexpr (V == 8) {
-            widen8<DT>(f.x, lo);
-            widen8<DT>(f.y, hi);
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) { lo[i] = f.lo[i]; hi[i] = f.hi[i]; }
-        }
-    }
-    __device__ __forceinline__ void load(const HeadnormArgs& a, const void* p, int64_t at, int l, int L, bool live) {
-        Fetched<DT, V, N, PAIRS> f;
-        f.load(a, p, at, l, L, live);
-        take(f);
     }
     __device__ __forceinline__ void store(const HeadnormArgs& a, void* p, int64_t at, int l, int L) const {
         if constexpr (V == 8) {
@@ -219,8 +200,9 @@ __global__ __launch_bounds__(kThreads) void k_headnorm(HeadnormArgs a, Rows w) {
 }
 
 // Backward.  A workgroup has some tokens of an example and all of one descriptor's heads: the gains' gradients of a lane's columns
-// stay in its registers.  `split` of its waves share a token's heads.  The next row's numbers are on their way while one is worked
-// on.  The sums go to partial[example][chunk][D] of the descriptor.
+// stay in its registers.  `split` of its waves share a token's heads.  The sums go to partial[example][chunk][D] of the descriptor.
+// (The next row's loads ahead of the present row's work made it slower, 89 us instead of 79 for 64 x 512 tokens of 12 + 12 heads of 64
+// bf16: the other waves' loads fill that time already, and the registers are theirs.)
 struct Back {
     Rows w;
     int tokens, chunks;        // of a workgroup, of an example
@@ -246,56 +228,41 @@ __global__ __launch_bounds__(kThreads) void k_headnorm_back(HeadnormArgs a, Back
     Row<0, V, N, PAIRS> acc = {}, gain;
     gain.load(a, hd.gain, 0, l, w.L, true);
     Turn<V, N> turn;
-    Fetched<DT, V, N, PAIRS> fx, fu;
     const int64_t x0 = b * hd.x_b, u0 = b * hd.dy_b, o0 = b * hd.o_b;
-    const int hl = g & (w.hw - 1);
-    int64_t n = t0 + wave / w.split * w.tw;            // the first of the wave's tokens; t the lane's
-    int it = it0;
-    const auto fetch = [&](int64_t n, int it) {
-        const int64_t t = n + g / w.hw;
-        const int h = it * w.hw + hl;
-        const bool live = t < end && h < hd.H;
-        fx.load(a, hd.x, x0 + t * hd.x_t + h * hd.x_h, l, w.L, live);
-        fu.load(a, hd.dy, u0 + t * hd.dy_t + h * hd.dy_h, l, w.L, live);
-    };
-    if (it0 < it1 && n < end) fetch(n, it);
-    while (it0 < it1 && n < end) {
-        const int64_t t = n + g / w.hw;
-        if (it == it0) {
-            const bool live = t < end;
-            const int position = !live ? 0 : a.positions ? a.positions[b * a.positions_b + t] : (int)t;
-            turn.of(a, position, l, w.L, live);
-        }
-        Row<DT, V, N, PAIRS> x, u;
-        x.take(fx);
-        u.take(fu);
-        const int h = it * w.hw + hl;
-        const bool live = t < end && h < hd.H;
-        if (++it == it1) { it = it0; n += step; }
-        if (n < end) fetch(n, it);
-        float sq = 0.f;
+    for (int64_t n = t0 + wave / w.split * w.tw; n < end; n += step) {
+        const int64_t t = n + g / w.hw;                // the lane's token
+        const bool here = t < end;
+        turn.of(a, !here ? 0 : a.positions ? a.positions[b * a.positions_b + t] : (int)t, l, w.L, here);
+        for (int it = it0; it < it1; ++it) {
+            const int h = it * w.hw + (g & (w.hw - 1));
+            const bool live = here && h < hd.H;
+            Row<DT, V, N, PAIRS> x, u;
+            x.load(a, hd.x, x0 + t * hd.x_t + h * hd.x_h, l, w.L, live);
+            u.load(a, hd.dy, u0 + t * hd.dy_t + h * hd.dy_h, l, w.L, live);
+            float sq = 0.f;
 #pragma unroll
-        for (int i = 0; i < V * N; ++i) sq += x.lo[i] * x.lo[i] + x.hi[i] * x.hi[i];
-        const float r = 1.0f / sqrtf(row_sum(sq, w.L) * mean + a.eps);
-        u.rotate(turn.s, turn.c, -1.0f);
-        float dot = 0.f;
+            for (int i = 0; i < V * N; ++i) sq += x.lo[i] * x.lo[i] + x.hi[i] * x.hi[i];
+            const float r = 1.0f / sqrtf(row_sum(sq, w.L) * mean + a.eps);
+            u.rotate(turn.s, turn.c, -1.0f);
+            float dot = 0.f;
 #pragma unroll
-        for (int i = 0; i < V * N; ++i) {
-            x.lo[i] *= r;
-            x.hi[i] *= r;
-            acc.lo[i] += u.lo[i] * x.lo[i];
-            acc.hi[i] += u.hi[i] * x.hi[i];
-            u.lo[i] *= gain.lo[i];
-            u.hi[i] *= gain.hi[i];
-            dot += u.lo[i] * x.lo[i] + u.hi[i] * x.hi[i];
-        }
-        dot = row_sum(dot, w.L) * mean;
+            for (int i = 0; i < V * N; ++i) {
+                x.lo[i] *= r;
+                x.hi[i] *= r;
+                acc.lo[i] += u.lo[i] * x.lo[i];
+                acc.hi[i] += u.hi[i] * x.hi[i];
+                u.lo[i] *= gain.lo[i];
+                u.hi[i] *= gain.hi[i];
+                dot += u.lo[i] * x.lo[i] + u.hi[i] * x.hi[i];
+            }
+            dot = row_sum(dot, w.L) * mean;
 #pragma unroll
-        for (int i = 0; i < V * N; ++i) {
-            x.lo[i] = r * (u.lo[i] - x.lo[i] * dot);
-            x.hi[i] = r * (u.hi[i] - x.hi[i] * dot);
+            for (int i = 0; i < V * N; ++i) {
+                x.lo[i] = r * (u.lo[i] - x.lo[i] * dot);
+                x.hi[i] = r * (u.hi[i] - x.hi[i] * dot);
+            }
+            if (live) x.store(a, hd.out, o0 + t * hd.o_t + h * hd.o_h, l, w.L);
         }
-        if (live) x.store(a, hd.out, o0 + t * hd.o_t + h * hd.o_h, l, w.L);
     }
     // the rows of a wave, then the waves, in a fixed order
 #pragma unroll
@@ -310,25 +277,27 @@ __global__ __launch_bounds__(kThreads) void k_headnorm_back(HeadnormArgs a, Back
         bk.partial[(int64_t)wg * a.D + j] = (sums[0][j] + sums[1][j]) + (sums[2][j] + sums[3][j]);
 }
 
-// A workgroup per example: the chunks' sums, by groups of threads for as many columns (W next to each other for a thread), and the
-// squared norm of the rows.
+// A workgroup per example: the chunks' sums (W columns next to each other for a thread, up to 64 threads along the columns, the
+// others take other chunks), and the squared norm of the rows.
 constexpr int kFoldThreads = 1024;
 template <int W>
 __global__ __launch_bounds__(kFoldThreads) void k_headnorm_fold(HeadnormArgs a, BackPlan plan, int accumulate, float* __restrict__ sqnorm) {
-    __shared__ double part[kFoldThreads][W];
-    __shared__ double red[kFoldThreads / kWave];
-    const int b = blockIdx.x, columns = a.D / W;
+    constexpr int kWaves = kFoldThreads / kWave;
+    __shared__ double part[kWaves][kWave * W];
+    __shared__ double red[kWaves];
+    const int b = blockIdx.x, columns = a.D / W, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
     int ct = 1;                                        // threads along the columns, a power of two
-    while (ct < columns && ct < kFoldThreads) ct *= 2;
-    const int groups = kFoldThreads / ct, c = threadIdx.x & (ct - 1), g = threadIdx.x / ct;
+    while (ct < columns && ct < kWave) ct *= 2;
+    const int groups = kFoldThreads / ct, g = threadIdx.x / ct;
     double sq = 0.0;
-    for (int which = 0; which < a.n_heads; ++which) {
-        const Back& bk = plan.of[which];
-        const float* p = bk.partial + (int64_t)b * bk.chunks * a.D + c * W;
-        double s[W];
+    for (int c0 = 0; c0 < columns; c0 += ct) {
+        const int c = c0 + (lane & (ct - 1));
+        double s[2][W] = {};
 #pragma unroll
-        for (int v = 0; v < W; ++v) s[v] = 0.0;
-        if (c < columns) {
+        for (int which = 0; which < 2; ++which) {
+            if (which >= a.n_heads || c >= columns) continue;
+            const Back& bk = plan.of[which];
+            const float* p = bk.partial + (int64_t)b * bk.chunks * a.D + c * W;
             int k = g;
             for (; k + 3 * groups < bk.chunks; k += 4 * groups) {
                 float f[4][W];
@@ -339,34 +308,39 @@ __global__ __launch_bounds__(kFoldThreads) void k_headnorm_fold(HeadnormArgs a, 
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int v = 0; v < W; ++v) s[v] += f[i][v];
+                    for (int v = 0; v < W; ++v) s[which][v] += f[i][v];
             }
             for (; k < bk.chunks; k += groups)
 #pragma unroll
-                for (int v = 0; v < W; ++v) s[v] += p[(int64_t)k * a.D + v];
+                for (int v = 0; v < W; ++v) s[which][v] += p[(int64_t)k * a.D + v];
         }
-        __syncthreads();
 #pragma unroll
-        for (int v = 0; v < W; ++v) part[threadIdx.x][v] = s[v];
-        __syncthreads();
-        if (g == 0 && c < columns) {
-            for (int k = 1; k < groups; ++k)
-#pragma unroll
-                for (int v = 0; v < W; ++v) s[v] += part[k * ct + c][v];
+        for (int which = 0; which < 2; ++which) {
+            if (which >= a.n_heads) break;
 #pragma unroll
             for (int v = 0; v < W; ++v) {
-                const float f = (float)s[v];
-                a.heads[which].gain_rows[(int64_t)b * a.D + c * W + v] = f;
+                for (int off = ct; off < kWave; off <<= 1) s[which][v] += __shfl_xor(s[which][v], off, kWave);
+                if (lane < ct) part[wave][lane * W + v] = s[which][v];
+            }
+            __syncthreads();
+            const int j = c0 * W + threadIdx.x;        // the column that this thread adds up over the waves
+            if ((int)threadIdx.x < ct * W && j < a.D) {
+                double sum = 0.0;
+#pragma unroll
+                for (int k = 0; k < kWaves; ++k) sum += part[k][threadIdx.x];
+                const float f = (float)sum;
+                a.heads[which].gain_rows[(int64_t)b * a.D + j] = f;
                 sq += (double)f * f;
             }
+            __syncthreads();
         }
     }
     sq = wave_sum_f64(sq);
-    if ((threadIdx.x & (kWave - 1)) == 0) red[threadIdx.x >> 6] = sq;
+    if (lane == 0) red[wave] = sq;
     __syncthreads();
     if (threadIdx.x != 0) return;
 #pragma unroll
-    for (int k = 1; k < kFoldThreads / kWave; ++k) sq += red[k];
+    for (int k = 1; k < kWaves; ++k) sq += red[k];
     sqnorm[b] = (float)(accumulate ? sqnorm[b] + sq : sq);
 }
 
