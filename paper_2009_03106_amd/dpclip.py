@@ -652,15 +652,26 @@ def add_noise(grad: torch.Tensor, stddev: float, seed: int, offset: int = 0, *,
     return grad
 
 
-def _here(device: torch.device, stream: Optional[torch.cuda.Stream], *tensors) -> None:
-    """The kernels run on the current device: every tensor, and the stream, has to belong to it."""
-    if device.type != "cuda":
-        raise ValueError("tensors must be contiguous device tensors")
-    if device.index != torch.cuda.current_device() or (stream is not None and stream.device.index != device.index):
-        raise ValueError(f"tensors and stream must be on the current device, not on {device}")
+def _here(stream: Optional[torch.cuda.Stream], *tensors) -> int:
+    """The kernels run on the current device: every tensor, and the stream, has to belong to it.  Returns its index."""
+    dev = torch._C._cuda_getDevice() if torch.cuda.is_initialized() else torch.cuda.current_device()
+    if stream is not None and stream.device.index != dev:
+        raise ValueError(f"the stream must be one of the current device, cuda:{dev}")
     for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError(f"tensors are on {device} and on {t.device}")
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"tensors must be on the current device, cuda:{dev}, not on {t.device}")
+    return dev
+
+
+def _vec(t: Optional[torch.Tensor], dtype: torch.dtype, n: int, name: str) -> Optional[int]:
+    """Address of a contiguous tensor of n elements (on the current device: _here)."""
+    if t is None:
+        return None
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or not t.is_contiguous():
+        raise TypeError(f"{name} must be a contiguous {dtype} device tensor")
+    if t.numel() != n:
+        raise ValueError(f"{name} must hold {n} elements, got {tuple(t.shape)}")
+    return t.data_ptr() if n > 0 else None
 
 
 def _made_on(stream: Optional[torch.cuda.Stream]):
@@ -676,6 +687,10 @@ class TensorDescs(NamedTuple):
     arr: object                     # ctypes array of dp_tensor_desc
     device: torch.device
     outs: Optional[list]            # the outputs, where the descriptors name any
+
+    def here(self) -> None:
+        if self.device.index != torch._C._cuda_getDevice():
+            raise ValueError(f"descriptors are of {self.device}, not of the current device")
 
 
 def tensor_descs(tensors, outs=None, *, in_place: bool = False) -> TensorDescs:
@@ -728,7 +743,8 @@ def tensors_norm(tensors, norm: Optional[torch.Tensor] = None, *, accumulate: bo
     n = len(descs.arr)
     if norm is None and accumulate:
         raise ValueError("accumulate needs an existing norm tensor")
-    _here(descs.device, stream, norm, tensor_norms, workspace)
+    _here(stream, norm, tensor_norms, workspace)
+    descs.here()
     with _made_on(stream):
         if norm is None:
             norm = torch.empty(1, dtype=torch.float32, device=descs.device)
@@ -749,7 +765,8 @@ def tensors_clip(tensors, norm: torch.Tensor, C: float, outs=None, *, accumulate
         if accumulate and outs is None:
             raise ValueError("accumulate needs existing outs")
         descs = tensor_descs(tensors, outs, in_place=outs is None)
-    _here(descs.device, stream, norm, workspace)
+    _here(stream, norm, workspace)
+    descs.here()
     with _made_on(stream):
         ws = _workspace(lambda: tensors_workspace_bytes(descs), descs.device, workspace)
     st = lib.dp_tensors_clip(descs.arr, len(descs.arr), _f32(norm, (1,), "norm"), float(C), int(bool(accumulate)),
@@ -769,7 +786,8 @@ def tensors_norm_clip(tensors, C: float, outs=None, *, accumulate: bool = False,
             raise ValueError("accumulate needs existing outs")
         descs = tensor_descs(tensors, outs, in_place=outs is None)
     n = len(descs.arr)
-    _here(descs.device, stream, norm, tensor_norms, workspace)
+    _here(stream, norm, tensor_norms, workspace)
+    descs.here()
     with _made_on(stream):
         if norm is None:
             norm = torch.empty(1, dtype=torch.float32, device=descs.device)
@@ -801,16 +819,6 @@ def relative_buckets(n_buckets: int, reach: int, both: bool = True, device="cuda
     return torch.tensor(back[::-1] + ahead[1:], dtype=torch.int32, device=device)
 
 
-def _i32(t: Optional[torch.Tensor], n: int, name: str) -> Optional[int]:
-    if t is None:
-        return None
-    if not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous():
-        raise TypeError(f"{name} must be a contiguous int32 device tensor")
-    if t.numel() != n:
-        raise ValueError(f"{name} must hold {n} elements, got {tuple(t.shape)}")
-    return t.data_ptr() if n > 0 else None
-
-
 def _inner(t: torch.Tensor, dims: int, name: str) -> int:
     """Address of a device tensor whose last dimension's elements are next to each other."""
     if not t.is_cuda or t.dim() != dims or (t.shape[-1] > 1 and t.stride(-1) != 1):
@@ -827,8 +835,9 @@ def _posbias_desc(x: torch.Tensor, out: Optional[torch.Tensor], buckets, n_bucke
     n = buckets.numel() if isinstance(buckets, torch.Tensor) else 0
     if n % 2 == 0:
         raise ValueError("buckets must hold one for each distance from -reach to reach")
-    return PosbiasDesc(B, H, Tq, Tk, s[0], s[1], s[2], o[0], o[1], o[2], _i32(buckets, n, "buckets"), n // 2, int(n_buckets),
-                       _i32(q_start, B, "q_start"), _i32(q_lens, B, "q_lens"), _i32(k_lens, B, "k_lens"), int(bool(causal)))
+    return PosbiasDesc(B, H, Tq, Tk, s[0], s[1], s[2], o[0], o[1], o[2], _vec(buckets, torch.int32, n, "buckets"), n // 2, int(n_buckets),
+                       _vec(q_start, torch.int32, B, "q_start"), _vec(q_lens, torch.int32, B, "q_lens"),
+                       _vec(k_lens, torch.int32, B, "k_lens"), int(bool(causal)))
 
 
 def posbias_add(scores: torch.Tensor, table: torch.Tensor, buckets: torch.Tensor, out: Optional[torch.Tensor] = None, *,
@@ -847,7 +856,7 @@ def posbias_add(scores: torch.Tensor, table: torch.Tensor, buckets: torch.Tensor
         raise ValueError("out must have the shape and the dtype of scores")
     if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.shape[1] != scores.shape[1]:
         raise ValueError("table must be [n_buckets, H]")
-    _here(scores.device, stream, out, table, buckets, q_start, q_lens, k_lens)
+    _here(stream, scores, out, table, buckets, q_start, q_lens, k_lens)
     d = _posbias_desc(scores, out, buckets, table.shape[0], q_start, q_lens, k_lens, causal)
     st = lib.dp_posbias_add(ctypes.byref(d), xp, _f32(table, table.shape, "table"), _dtype_code(scores), op, _stream_ptr(stream))
     _check(st, "dp_posbias_add")
@@ -870,7 +879,7 @@ def posbias_sqnorm(dS: torch.Tensor, buckets: torch.Tensor, n_buckets: int, sqno
     B, H = dS.shape[0], dS.shape[1]
     if sqnorm is None and accumulate:
         raise ValueError("accumulate needs an existing sqnorm tensor")
-    _here(dS.device, stream, sqnorm, rows, buckets, q_start, q_lens, k_lens, workspace)
+    _here(stream, dS, sqnorm, rows, buckets, q_start, q_lens, k_lens, workspace)
     d = _posbias_desc(dS, None, buckets, n_buckets, q_start, q_lens, k_lens, causal)
     with _made_on(stream):
         if sqnorm is None:
@@ -893,6 +902,10 @@ class HeadDescs(NamedTuple):
     dtype: int
     outs: list
     gain_rows: Optional[list]
+
+    def here(self) -> None:
+        if self.device.index != torch._C._cuda_getDevice():
+            raise ValueError(f"descriptors are of {self.device}, not of the current device")
 
 
 def rotary_freqs(rot: int, base: float = 10000.0, device="cuda") -> torch.Tensor:
@@ -943,9 +956,9 @@ def _headnorm_desc(d: HeadDescs, freqs, positions, lengths, pairs, eps) -> Headn
     pp, pb = None, 0
     if positions is not None:
         pb = d.T if positions.dim() == 2 else 0
-        pp = _i32(positions, d.B * d.T if positions.dim() == 2 else d.T, "positions")
+        pp = _vec(positions, torch.int32, d.B * d.T if positions.dim() == 2 else d.T, "positions")
     return HeadnormDesc(d.B, d.T, d.D, rot, int(bool(pairs)), float(eps), pp, pb, freqs.data_ptr() if rot else None,
-                        _i32(lengths, d.B, "lengths"))
+                        _vec(lengths, torch.int32, d.B, "lengths"))
 
 
 def headnorm(heads, outs=None, *, freqs: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
@@ -964,7 +977,8 @@ def headnorm(heads, outs=None, *, freqs: Optional[torch.Tensor] = None, position
                 make = torch.empty if lengths is None else torch.zeros
                 outs = [make(x.shape, dtype=x.dtype, device=x.device) for x, _ in heads]
         descs = head_descs(heads, outs)
-    _here(descs.device, stream, freqs, positions, lengths)
+    _here(stream, freqs, positions, lengths)
+    descs.here()
     d = _headnorm_desc(descs, freqs, positions, lengths, pairs, eps)
     st = lib.dp_headnorm(ctypes.byref(d), descs.arr, len(descs.arr), descs.dtype, _stream_ptr(stream))
     _check(st, "dp_headnorm")
@@ -1000,7 +1014,8 @@ def headnorm_sqnorm(heads, dys, sqnorm: Optional[torch.Tensor] = None, outs=None
         if sqnorm is None:
             sqnorm = torch.empty(descs.B, dtype=torch.float32, device=descs.device)
         ws = _workspace(lambda: headnorm_workspace_bytes(descs), descs.device, workspace)
-    _here(descs.device, stream, sqnorm, freqs, positions, lengths, workspace)
+    _here(stream, sqnorm, freqs, positions, lengths, workspace)
+    descs.here()
     d = _headnorm_desc(descs, freqs, positions, lengths, pairs, eps)
     st = lib.dp_headnorm_sqnorm(ctypes.byref(d), descs.arr, len(descs.arr), descs.dtype, int(bool(accumulate)),
                                 _f32(sqnorm, (descs.B,), "sqnorm"), *_ws_args(ws), _stream_ptr(stream))
