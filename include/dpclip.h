@@ -519,7 +519,7 @@ typedef struct {
 } dp_heads_desc;
 
 typedef struct {
-    int64_t B, T, D;           /* D at most 1024 */
+    int64_t B, T, D;           /* D at most 512 */
     int64_t rot;               /* even, 0 to D */
     dp_rotation rotation;
     float eps;                 /* > 0 */

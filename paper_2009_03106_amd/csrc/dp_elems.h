@@ -51,20 +51,24 @@ template <int DT> __device__ __forceinline__ void widen8(const Raw8<DT>& r, floa
     }
 }
 template <int DT> __device__ __forceinline__ void load8(const void* p, int64_t k, float (&v)[8]) { widen8<DT>(load_raw8<DT>(p, k), v); }
-// rounded to nearest, ties to even
-template <int DT> __device__ __forceinline__ void store8(void* p, int64_t k, const float (&v)[8]) {
+// rounded to nearest, ties to even; PAST: past the caches, for outputs that do not fit them
+template <bool PAST, class T> __device__ __forceinline__ void store_raw(const T& v, Global<T>* p) {
+    if constexpr (PAST) __builtin_nontemporal_store(v, p);
+    else *p = v;
+}
+template <int DT, bool PAST = false> __device__ __forceinline__ void store8(void* p, int64_t k, const float (&v)[8]) {
     if constexpr (DT == 0) {
         Global<u32x4_any4>* q = global_out<u32x4_any4>(static_cast<float*>(p) + k);
         u32x4_any4 a, b;
 #pragma unroll
         for (int j = 0; j < 4; ++j) { a[j] = __float_as_uint(v[j]); b[j] = __float_as_uint(v[4 + j]); }
-        q[0] = a;
-        q[1] = b;
+        store_raw<PAST>(a, q);
+        store_raw<PAST>(b, q + 1);
     } else {
         u32x4_any2 a;
 #pragma unroll
         for (int j = 0; j < 4; ++j) a[j] = In16<DT == 2>::pack(v[2 * j], v[2 * j + 1]);
-        *global_out<u32x4_any2>(static_cast<uint16_t*>(p) + k) = a;
+        store_raw<PAST>(a, global_out<u32x4_any2>(static_cast<uint16_t*>(p) + k));
     }
 }
 

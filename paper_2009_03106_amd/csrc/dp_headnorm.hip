@@ -21,78 +21,96 @@ struct Rows {
     int split;                 // waves that share a token's steps
 };
 
-// The pairs of a row: V next to each other at a time, N times for a lane.
-//   V == 1: pair l + i L for lane l, any D and rot
-//   V == 8: pairs 8 l to 8 l + 7, D and rot multiples of 16: two pieces of eight numbers (16 bytes; float32: 32) for a lane
-// PAIRS (V == 8): neighbours turn together, the pieces are next to each other; else they are half of `rot` apart, and next to
-// each other behind the numbers that turn.
-__device__ __forceinline__ int2 columns(const HeadnormArgs& a, int p) {
-    if (a.pairs) return make_int2(2 * p, 2 * p + 1);
-    const int half = a.rot / 2;
-    return p < half ? make_int2(p, p + half) : make_int2(2 * p, 2 * p + 1);
-}
-template <bool PAIRS> __device__ __forceinline__ int2 pieces(const HeadnormArgs& a, int l) {
-    const int half = a.rot / 2;
-    return PAIRS || 8 * l >= half ? make_int2(16 * l, 16 * l + 8) : make_int2(8 * l, 8 * l + half);
+// A lane has two pieces of eight numbers (16 bytes; float32: 32), eight pairs.
+//   halves: columns 8 l and rot / 2 + 8 l, as far as the numbers turn; behind them 16 numbers next to each other
+//   PAIRS:  columns 16 l to 16 l + 15, neighbours turn together
+// na, nb: how many of each piece there are (WHOLE: eight, or none for lanes behind the row).
+struct Pieces { int a, b, na, nb; };
+template <bool PAIRS, bool WHOLE> __device__ __forceinline__ Pieces pieces(const HeadnormArgs& a, int l) {
+    const int half = a.rot / 2, turning = PAIRS ? 0 : (half + 7) / 8;      // lanes with pairs that are half of `rot` apart
+    Pieces p;
+    if (!PAIRS && l < turning) {
+        p.a = 8 * l;
+        p.b = half + 8 * l;
+        p.na = p.nb = WHOLE ? 8 : min(8, half - 8 * l);
+    } else {
+        p.a = (PAIRS ? 0 : a.rot) + 16 * (l - turning);
+        p.b = p.a + 8;
+        p.na = WHOLE ? (p.a < a.D ? 8 : 0) : min(8, max(0, a.D - p.a));
+        p.nb = WHOLE ? p.na : min(8, max(0, a.D - p.b));
+    }
+    return p;
 }
 
-template <int DT, int V, int N, bool PAIRS> struct Row {
-    float lo[V * N], hi[V * N];            // (lo[i], hi[i]) turn together; PAIRS: neighbours within lo, and within hi
+// n numbers of the row at `row`, from column c on.  A piece that is not whole is the end of eight numbers (where the row has as many
+// before its end), moved to the front: one load, and selects.
+template <int DT, bool WHOLE> __device__ __forceinline__ void load_some(const void* p, int64_t row, int c, int n, float (&v)[8]) {
+    if constexpr (WHOLE) {
+        Raw8<DT> r{};
+        if (n) r = load_raw8<DT>(p, row + c);
+        widen8<DT>(r, v);
+    } else if (n == 0 || c + n >= 8) {
+        const int over = 8 - n;
+        Raw8<DT> r{};
+        if (n) r = load_raw8<DT>(p, row + c - over);
+        widen8<DT>(r, v);
+        if (__ballot(over & 7)) {
+            const bool four = over & 4, two = over & 2, one = over & 1;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) { const float u = j < 4 ? v[(j + 4) & 7] : 0.f; v[j] = four ? u : v[j]; }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) { const float u = j < 6 ? v[(j + 2) & 7] : 0.f; v[j] = two ? u : v[j]; }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) { const float u = j < 7 ? v[(j + 1) & 7] : 0.f; v[j] = one ? u : v[j]; }
+        }
+    } else {
+        load_first<DT>(p, row + c, n, v);
+    }
+}
+template <int DT, bool WHOLE> __device__ __forceinline__ void store_some(void* p, int64_t at, int n, const float (&v)[8]) {
+    if (n == 8)      store8<DT>(p, at, v);
+    else if (!WHOLE) store_first<DT>(p, at, n, f32x8{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]});
+}
+
+template <int DT, bool PAIRS, bool WHOLE> struct Row {
+    float lo[8], hi[8];        // (lo[i], hi[i]) turn together; PAIRS: neighbours within lo, and within hi
 
     // zeros where there are none
-    __device__ __forceinline__ void load(const HeadnormArgs& a, const void* p, int64_t at, int l, int L, bool live) {
-        if constexpr (V == 8) {
-            const int2 c = pieces<PAIRS>(a, l);
-            Raw8<DT> x{}, y{};
-            if (live && 16 * l < a.D) {
-                x = load_raw8<DT>(p, at + c.x);
-                y = load_raw8<DT>(p, at + c.y);
-            }
-            widen8<DT>(x, lo);
-            widen8<DT>(y, hi);
-        } else {
+    __device__ __forceinline__ void load(const Pieces& c, const void* p, int64_t at, bool live) {
+        load_some<DT, WHOLE>(p, at, c.a, live ? c.na : 0, lo);
+        load_some<DT, WHOLE>(p, at, c.b, live ? c.nb : 0, hi);
+    }
+    __device__ __forceinline__ void store(const Pieces& c, void* p, int64_t at) const {
+        store_some<DT, WHOLE>(p, at + c.a, c.na, lo);
+        store_some<DT, WHOLE>(p, at + c.b, c.nb, hi);
+    }
+    __device__ __forceinline__ void to_lds(const Pieces& c, float* row) const {
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int2 c = columns(a, l + i * L);
-                lo[i] = live && c.x < a.D ? load_one<DT>(p, at + c.x) : 0.f;
-                hi[i] = live && c.y < a.D ? load_one<DT>(p, at + c.y) : 0.f;
-            }
+        for (int i = 0; i < 8; ++i) {
+            if (i < c.na) row[c.a + i] = lo[i];
+            if (i < c.nb) row[c.b + i] = hi[i];
         }
     }
-    __device__ __forceinline__ void store(const HeadnormArgs& a, void* p, int64_t at, int l, int L) const {
-        if constexpr (V == 8) {
-            const int2 c = pieces<PAIRS>(a, l);
-            if (16 * l < a.D) {
-                store8<DT>(p, at + c.x, lo);
-                store8<DT>(p, at + c.y, hi);
+    __device__ __forceinline__ void from_lds(const Pieces& c, const float* row) {
+        if constexpr (WHOLE) {                         // pieces begin on 32 bytes; lanes behind the row read a piece and drop it
+            const float4* p = reinterpret_cast<const float4*>(row + (c.na ? c.a : 0));
+            const float4* q = reinterpret_cast<const float4*>(row + (c.na ? c.b : 0));
+            const float4 f[4] = {p[0], p[1], q[0], q[1]};
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                lo[4 * i] = f[i].x; lo[4 * i + 1] = f[i].y; lo[4 * i + 2] = f[i].z; lo[4 * i + 3] = f[i].w;
+                hi[4 * i] = f[2 + i].x; hi[4 * i + 1] = f[2 + i].y; hi[4 * i + 2] = f[2 + i].z; hi[4 * i + 3] = f[2 + i].w;
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int2 c = columns(a, l + i * L);
-                if (c.x < a.D) store_one<DT>(p, at + c.x, lo[i]);
-                if (c.y < a.D) store_one<DT>(p, at + c.y, hi[i]);
-            }
-        }
-    }
-    __device__ __forceinline__ void to_lds(const HeadnormArgs& a, float* row, int l, int L) const {
-        if constexpr (V == 8) {
-            const int2 c = pieces<PAIRS>(a, l);
-            if (16 * l < a.D) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) { row[c.x + i] = lo[i]; row[c.y + i] = hi[i]; }
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                const int2 c = columns(a, l + i * L);
-                if (c.x < a.D) row[c.x] = lo[i];
-                if (c.y < a.D) row[c.y] = hi[i];
+            for (int i = 0; i < 8; ++i) {
+                lo[i] = i < c.na ? row[c.a + i] : 0.f;
+                hi[i] = i < c.nb ? row[c.b + i] : 0.f;
             }
         }
     }
     // the pairs, by the angles whose sines and cosines these are (sign -1: back)
-    __device__ __forceinline__ void rotate(const float (&s)[V * N], const float (&c)[V * N], float sign) {
+    __device__ __forceinline__ void rotate(const float (&s)[8], const float (&c)[8], float sign) {
         const auto one = [&](float& x, float& y, int k) {
             const float sk = sign * s[k], t = x * c[k] - y * sk;
             y = x * sk + y * c[k];
@@ -103,19 +121,19 @@ template <int DT, int V, int N, bool PAIRS> struct Row {
             for (int i = 0; i < 4; ++i) { one(lo[2 * i], lo[2 * i + 1], i); one(hi[2 * i], hi[2 * i + 1], 4 + i); }
         } else {
 #pragma unroll
-            for (int i = 0; i < V * N; ++i) one(lo[i], hi[i], i);
+            for (int i = 0; i < 8; ++i) one(lo[i], hi[i], i);
         }
     }
 };
 
-// sine and cosine of position * freq.  The angle is taken in turns and in 64 bits: what is left of it after the whole quarters is
-// at most an eighth of a turn, exact to 2^-53 of the position's turns, and the series below are exact to float32 there (the first
-// terms left out: x^11 / 11! < 2e-9, x^12 / 12! < 2e-10 for x up to pi / 4).
+// sine and cosine of position * freq.  The angle is taken in turns and in 64 bits, without its whole turns and then without its
+// nearest quarter: what is left is at most an eighth of a turn, and the series below are exact to float32 there (the first terms
+// left out: x^11 / 11! < 2e-9, x^12 / 12! < 2e-10 for x up to pi / 4).
 __device__ __forceinline__ void sincos_of(int position, double freq, float& s, float& c) {
-    const double turns = (double)position * (freq * 0.15915494309189533577);
-    const double quarters = rint(turns * 4.0);
-    const float x = (float)((turns - quarters * 0.25) * 6.283185307179586477);
-    const int q = (int)(int64_t)(quarters - 4.0 * floor(quarters * 0.25));          // 0 to 3
+    const double turns = (double)position * (freq * 0.15915494309189533577), part = turns - floor(turns);      // 0 to 1
+    const double quarter = rint(part * 4.0);
+    const float x = (float)(part - quarter * 0.25) * 6.2831853f;
+    const int q = (int)quarter & 3;
     const float z = x * x;
     const float sx = x + x * z * (-1.6666667e-1f + z * (8.3333333e-3f + z * (-1.9841270e-4f + z * 2.7557319e-6f)));
     const float cx = 1.0f + z * (-0.5f + z * (4.1666667e-2f + z * (-1.3888889e-3f + z * (2.4801587e-5f + z * -2.7557319e-7f))));
@@ -125,19 +143,16 @@ __device__ __forceinline__ void sincos_of(int position, double freq, float& s, f
     if (q == 1 || q == 2) c = -c;
 }
 
-// the turn of each pair of a lane; pairs behind the rotated ones do not turn
-template <int V, int N> struct Turn {
-    float s[V * N], c[V * N];
-    __device__ __forceinline__ void of(const HeadnormArgs& a, int position, int l, int L, bool live) {
+// the turn of each pair of a lane, pairs 8 l to 8 l + 7; those behind the rotated ones do not turn
+struct Turn {
+    float s[8], c[8];
+    __device__ __forceinline__ void of(const HeadnormArgs& a, int position, int l, bool live) {
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int p = (l + i * L) * V + v, k = i * V + v;
-                s[k] = 0.f;
-                c[k] = 1.f;
-                if (live && p < a.rot / 2) sincos_of(position, a.freqs[p], s[k], c[k]);
-            }
+        for (int v = 0; v < 8; ++v) {
+            s[v] = 0.f;
+            c[v] = 1.f;
+            if (live && 8 * l + v < a.rot / 2) sincos_of(position, a.freqs[8 * l + v], s[v], c[v]);
+        }
     }
 };
 
@@ -159,41 +174,42 @@ __device__ __forceinline__ Token token_of(const HeadnormArgs& a, int64_t n) {
 }
 
 // A wave takes tw tokens at a time and its share of the steps over their heads.
-template <int DT, int V, int N, bool PAIRS>
+template <int DT, bool PAIRS, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void k_headnorm(HeadnormArgs a, Rows w) {
     const int lane = threadIdx.x & (kWave - 1), l = lane & (w.L - 1), g = lane / w.L;
     const int64_t wave = (int64_t)blockIdx.x * (kThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t step = (int64_t)gridDim.x * (kThreads / kWave) / w.split;
     const int part = (int)(wave % w.split);
     const int it0 = (int)((int64_t)w.its * part / w.split), it1 = (int)((int64_t)w.its * (part + 1) / w.split);
+    const Pieces pc = pieces<PAIRS, WHOLE>(a, l);
     const float mean = 1.0f / a.D;
     for (int64_t n0 = wave / w.split * w.tw; n0 < (int64_t)a.B * a.T; n0 += step * w.tw) {
         const Token k = token_of(a, n0 + g / w.hw);
-        Turn<V, N> turn;
-        turn.of(a, k.position, l, w.L, k.live);
+        Turn turn;
+        turn.of(a, k.position, l, k.live);
 #pragma unroll 1
         for (int which = it0 >= w.its0; which <= (it1 > w.its0); ++which) {
             const HeadsArgs& hd = a.heads[which];
             const int first = which ? w.its0 : 0, from = max(it0, first), to = which ? it1 : min(it1, w.its0);
-            Row<0, V, N, PAIRS> gain;
-            gain.load(a, hd.gain, 0, l, w.L, true);
+            Row<0, PAIRS, WHOLE> gain;
+            gain.load(pc, hd.gain, 0, true);
             const int64_t in = k.b * hd.x_b + k.t * hd.x_t, out = k.b * hd.o_b + k.t * hd.o_t;
             for (int it = from; it < to; ++it) {
                 const int h = (it - first) * w.hw + (g & (w.hw - 1));
                 const bool live = k.live && h < hd.H;
-                Row<DT, V, N, PAIRS> x;
-                x.load(a, hd.x, in + h * hd.x_h, l, w.L, live);
+                Row<DT, PAIRS, WHOLE> x;
+                x.load(pc, hd.x, in + h * hd.x_h, live);
                 float sq = 0.f;
 #pragma unroll
-                for (int i = 0; i < V * N; ++i) sq += x.lo[i] * x.lo[i] + x.hi[i] * x.hi[i];
-                const float r = 1.0f / sqrtf(row_sum(sq, w.L) * mean + a.eps);
+                for (int i = 0; i < 8; ++i) sq += x.lo[i] * x.lo[i] + x.hi[i] * x.hi[i];
+                const float r = rsqrtf(row_sum(sq, w.L) * mean + a.eps);
 #pragma unroll
-                for (int i = 0; i < V * N; ++i) {
+                for (int i = 0; i < 8; ++i) {
                     x.lo[i] *= r * gain.lo[i];
                     x.hi[i] *= r * gain.hi[i];
                 }
                 x.rotate(turn.s, turn.c, 1.0f);
-                if (live) x.store(a, hd.out, out + h * hd.o_h, l, w.L);
+                if (live) x.store(pc, hd.out, out + h * hd.o_h);
             }
         }
     }
@@ -210,9 +226,10 @@ struct Back {
 };
 struct BackPlan { Back of[2]; int first; };            // workgroups from `first` on have the second descriptor's heads
 
-template <int DT, int V, int N, bool PAIRS>
-__global__ __launch_bounds__(kThreads) void k_headnorm_back(HeadnormArgs a, BackPlan plan) {
+template <int DT, bool PAIRS, bool WHOLE>
+__global__ __launch_bounds__(kThreads, 3) void k_headnorm_back(HeadnormArgs a, BackPlan plan) {
     __shared__ float sums[kThreads / kWave][kMaxHeadDim];
+    __shared__ __align__(16) float gains[kMaxHeadDim]; // not in registers, which decide how many waves there are
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int which = (int)blockIdx.x >= plan.first;
     const Back& bk = plan.of[which];
@@ -224,29 +241,34 @@ __global__ __launch_bounds__(kThreads) void k_headnorm_back(HeadnormArgs a, Back
     const int64_t t0 = (int64_t)chunk * bk.tokens;
     const int end = (int)min(t0 + bk.tokens, (int64_t)(a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T));
     const int step = kThreads / kWave / w.split * w.tw;
+    const Pieces pc = pieces<PAIRS, WHOLE>(a, l);
     const float mean = 1.0f / a.D;
-    Row<0, V, N, PAIRS> acc = {}, gain;
-    gain.load(a, hd.gain, 0, l, w.L, true);
-    Turn<V, N> turn;
+    for (int j = threadIdx.x; j < a.D; j += kThreads) gains[j] = global_in<float>(hd.gain)[j];
+    __syncthreads();
+    Row<0, PAIRS, WHOLE> acc = {};
+    Turn turn;
     const int64_t x0 = b * hd.x_b, u0 = b * hd.dy_b, o0 = b * hd.o_b;
     for (int64_t n = t0 + wave / w.split * w.tw; n < end; n += step) {
         const int64_t t = n + g / w.hw;                // the lane's token
         const bool here = t < end;
-        turn.of(a, !here ? 0 : a.positions ? a.positions[b * a.positions_b + t] : (int)t, l, w.L, here);
+        turn.of(a, !here ? 0 : a.positions ? a.positions[b * a.positions_b + t] : (int)t, l, here);
         for (int it = it0; it < it1; ++it) {
             const int h = it * w.hw + (g & (w.hw - 1));
             const bool live = here && h < hd.H;
-            Row<DT, V, N, PAIRS> x, u;
-            x.load(a, hd.x, x0 + t * hd.x_t + h * hd.x_h, l, w.L, live);
-            u.load(a, hd.dy, u0 + t * hd.dy_t + h * hd.dy_h, l, w.L, live);
+            Row<DT, PAIRS, WHOLE> x, u;
+            x.load(pc, hd.x, x0 + t * hd.x_t + h * hd.x_h, live);
+            u.load(pc, hd.dy, u0 + t * hd.dy_t + h * hd.dy_h, live);
             float sq = 0.f;
 #pragma unroll
-            for (int i = 0; i < V * N; ++i) sq += x.lo[i] * x.lo[i] + x.hi[i] * x.hi[i];
-            const float r = 1.0f / sqrtf(row_sum(sq, w.L) * mean + a.eps);
+            for (int i = 0; i < 8; ++i) sq += x.lo[i] * x.lo[i] + x.hi[i] * x.hi[i];
+            const float r = rsqrtf(row_sum(sq, w.L) * mean + a.eps);
             u.rotate(turn.s, turn.c, -1.0f);
+            Row<0, PAIRS, WHOLE> gain;
+            asm volatile("" ::: "memory");             // else the reads move out of the loops, and into registers
+            gain.from_lds(pc, gains);
             float dot = 0.f;
 #pragma unroll
-            for (int i = 0; i < V * N; ++i) {
+            for (int i = 0; i < 8; ++i) {
                 x.lo[i] *= r;
                 x.hi[i] *= r;
                 acc.lo[i] += u.lo[i] * x.lo[i];
@@ -257,21 +279,21 @@ __global__ __launch_bounds__(kThreads) void k_headnorm_back(HeadnormArgs a, Back
             }
             dot = row_sum(dot, w.L) * mean;
 #pragma unroll
-            for (int i = 0; i < V * N; ++i) {
+            for (int i = 0; i < 8; ++i) {
                 x.lo[i] = r * (u.lo[i] - x.lo[i] * dot);
                 x.hi[i] = r * (u.hi[i] - x.hi[i] * dot);
             }
-            if (live) x.store(a, hd.out, o0 + t * hd.o_t + h * hd.o_h, l, w.L);
+            if (live) x.store(pc, hd.out, o0 + t * hd.o_t + h * hd.o_h);
         }
     }
     // the rows of a wave, then the waves, in a fixed order
 #pragma unroll
-    for (int i = 0; i < V * N; ++i)
+    for (int i = 0; i < 8; ++i)
         for (int off = w.L; off < kWave; off <<= 1) {
             acc.lo[i] += __shfl_xor(acc.lo[i], off, kWave);
             acc.hi[i] += __shfl_xor(acc.hi[i], off, kWave);
         }
-    if (g == 0) acc.to_lds(a, sums[wave], l, w.L);
+    if (g == 0) acc.to_lds(pc, sums[wave]);
     __syncthreads();
     for (int j = threadIdx.x; j < a.D; j += kThreads)
         bk.partial[(int64_t)wg * a.D + j] = (sums[0][j] + sums[1][j]) + (sums[2][j] + sums[3][j]);
@@ -350,19 +372,19 @@ int pow2_up(int n) {
     return p;
 }
 
-// pairs of a lane and lanes of a row
-struct Shape { int V, N, L; };
-// (16-byte pieces where D and rot are multiples of 16; numbers one by one took 500 us instead of the pieces' for
-// 4 x 8192 tokens of 32 + 8 heads of 128 bf16)
-Shape shape_of(const HeadnormArgs& a) {
-    if (a.D % 16 == 0 && a.rot % 16 == 0) return Shape{8, 1, pow2_up(a.D / 16)};
-    const int pairs = (a.D + 1) / 2, L = std::min(kWave, pow2_up(pairs));
-    return Shape{1, pow2_up((pairs + L - 1) / L), L};
+// lanes of a row: at most 34 have something of 512 numbers
+int lanes_of(const HeadnormArgs& a) {
+    return pow2_up(a.pairs ? ceil_div(a.D, 16) : ceil_div(a.rot / 2, 8) + ceil_div(a.D - a.rot, 16));
 }
+// Whether every lane's pieces are whole.  (Others take rows whose ends are loaded and stored in smaller pieces.  Numbers one by one
+// for those, a row per wave, took 173 us instead of 87 for the backward pass of 58 x 305 tokens of 8 + 8 heads of 110 bf16.)
+bool whole_pieces(const HeadnormArgs& a) { return a.D % 16 == 0 && (a.pairs || a.rot % 16 == 0); }
 
-// Heads and tokens of a wave: as many heads (which lie next to each other) as leave at most a tenth of the rows idle, else the
-// number with the fewest idle ones.
-Rows rows_of(int H0, int H1, int L) {
+constexpr int kTurns = 4;
+// Heads and tokens of a wave.  Heads lie next to each other, but the rows of a token have the same angles: as many heads at a time as
+// leave each lane `turns` steps over a token's heads, the number that leaves fewest rows idle (a tenth at most, if there is such a
+// one).  A token's angles cost about as much as working on a row.
+Rows rows_of(int H0, int H1, int L, int turns) {
     const int W = kWave / L;
     Rows w{};
     w.L = L;
@@ -370,7 +392,7 @@ Rows rows_of(int H0, int H1, int L) {
     for (int hw = W; hw >= 1; hw /= 2) {
         const int i0 = ceil_div(H0, hw), i1 = ceil_div(H1, hw);
         const int64_t taken = (int64_t)hw * (i0 + i1);
-        if (taken >= least) continue;
+        if (taken > least || (hw > 1 && i0 + i1 < turns)) continue;
         least = taken;
         w.hw = hw; w.tw = W / hw; w.its0 = i0; w.its = i0 + i1;
         if (taken * 10 <= (int64_t)(H0 + H1) * 11) break;
@@ -392,7 +414,7 @@ BackPlan plan_back(const HeadnormArgs& a, int L, float* partial) {
     int64_t steps = 0;                                  // of all waves together
     for (int i = 0; i < a.n_heads; ++i) {
         Rows& w = p.of[i].w;
-        w = rows_of(a.heads[i].H, 0, L);
+        w = rows_of(a.heads[i].H, 0, L, kTurns);
         steps += (int64_t)a.B * ceil_div(a.T, w.tw) * w.its;
     }
     const int64_t per_wave = std::max<int64_t>(1, steps / (kBackGroups * waves));
@@ -410,28 +432,19 @@ BackPlan plan_back(const HeadnormArgs& a, int L, float* partial) {
     return p;
 }
 
-template <int DT, int V, int N, bool PAIRS> void forward_as(const HeadnormArgs& a, const Rows& w, int grid, hipStream_t st) {
-    k_headnorm<DT, V, N, PAIRS><<<grid, kThreads, 0, st>>>(a, w);
+template <int DT, bool PAIRS, bool WHOLE> void forward_as(const HeadnormArgs& a, const Rows& w, int grid, hipStream_t st) {
+    k_headnorm<DT, PAIRS, WHOLE><<<grid, kThreads, 0, st>>>(a, w);
 }
-template <int DT, int V, int N, bool PAIRS> void backward_as(const HeadnormArgs& a, const BackPlan& p, hipStream_t st) {
-    k_headnorm_back<DT, V, N, PAIRS><<<a.B * (p.of[0].chunks + p.of[1].chunks), kThreads, 0, st>>>(a, p);
+template <int DT, bool PAIRS, bool WHOLE> void backward_as(const HeadnormArgs& a, const BackPlan& p, hipStream_t st) {
+    k_headnorm_back<DT, PAIRS, WHOLE><<<a.B * (p.of[0].chunks + p.of[1].chunks), kThreads, 0, st>>>(a, p);
 }
-
-template <int DT> void forward(const HeadnormArgs& a, const Shape& s, const Rows& w, int grid, hipStream_t st) {
-    if (s.V == 8 && a.pairs) forward_as<DT, 8, 1, true>(a, w, grid, st);
-    else if (s.V == 8) forward_as<DT, 8, 1, false>(a, w, grid, st);
-    else if (s.N == 1) forward_as<DT, 1, 1, false>(a, w, grid, st);
-    else if (s.N == 2) forward_as<DT, 1, 2, false>(a, w, grid, st);
-    else if (s.N == 4) forward_as<DT, 1, 4, false>(a, w, grid, st);
-    else               forward_as<DT, 1, 8, false>(a, w, grid, st);
+template <int DT> void forward(const HeadnormArgs& a, const Rows& w, int grid, hipStream_t st) {
+    if (whole_pieces(a)) a.pairs ? forward_as<DT, true, true>(a, w, grid, st) : forward_as<DT, false, true>(a, w, grid, st);
+    else                 a.pairs ? forward_as<DT, true, false>(a, w, grid, st) : forward_as<DT, false, false>(a, w, grid, st);
 }
-template <int DT> void backward(const HeadnormArgs& a, const Shape& s, const BackPlan& p, hipStream_t st) {
-    if (s.V == 8 && a.pairs) backward_as<DT, 8, 1, true>(a, p, st);
-    else if (s.V == 8) backward_as<DT, 8, 1, false>(a, p, st);
-    else if (s.N == 1) backward_as<DT, 1, 1, false>(a, p, st);
-    else if (s.N == 2) backward_as<DT, 1, 2, false>(a, p, st);
-    else if (s.N == 4) backward_as<DT, 1, 4, false>(a, p, st);
-    else               backward_as<DT, 1, 8, false>(a, p, st);
+template <int DT> void backward(const HeadnormArgs& a, const BackPlan& p, hipStream_t st) {
+    if (whole_pieces(a)) a.pairs ? backward_as<DT, true, true>(a, p, st) : backward_as<DT, false, true>(a, p, st);
+    else                 a.pairs ? backward_as<DT, true, false>(a, p, st) : backward_as<DT, false, false>(a, p, st);
 }
 
 }  // namespace
@@ -444,8 +457,7 @@ bool headnorm_fits(int64_t B, int64_t T, int64_t H0, int64_t H1) {
 size_t headnorm_ws_bytes(int n_heads, int B, int T, int D) { return (size_t)B * most_chunks(B, T) * n_heads * D * sizeof(float); }
 
 hipError_t launch_headnorm(const HeadnormArgs& a, int dt, hipStream_t st) {
-    const Shape s = shape_of(a);
-    Rows w = rows_of(a.heads[0].H, a.heads[1].H, s.L);
+    Rows w = rows_of(a.heads[0].H, a.heads[1].H, lanes_of(a), kTurns);
     // a wave for every tw tokens; where that leaves the chip empty, several waves share a token's heads
     const int64_t groups = ((int64_t)a.B * a.T + w.tw - 1) / w.tw;
     w.split = (int)std::max<int64_t>(1, std::min<int64_t>(w.its, 4096 / groups));
@@ -453,18 +465,17 @@ hipError_t launch_headnorm(const HeadnormArgs& a, int dt, hipStream_t st) {
     int grid = (int)std::min<int64_t>(wgs, 1 << 14);
     // whole tokens: a multiple of split waves
     while ((int64_t)grid * (kThreads / kWave) % w.split) ++grid;
-    if (dt == 0)      forward<0>(a, s, w, grid, st);
-    else if (dt == 1) forward<1>(a, s, w, grid, st);
-    else              forward<2>(a, s, w, grid, st);
+    if (dt == 0)      forward<0>(a, w, grid, st);
+    else if (dt == 1) forward<1>(a, w, grid, st);
+    else              forward<2>(a, w, grid, st);
     return hipGetLastError();
 }
 
 hipError_t launch_headnorm_sqnorm(const HeadnormArgs& a, int dt, bool accumulate, float* sqnorm, void* ws, hipStream_t st) {
-    const Shape s = shape_of(a);
-    const BackPlan p = plan_back(a, s.L, static_cast<float*>(ws));
-    if (dt == 0)      backward<0>(a, s, p, st);
-    else if (dt == 1) backward<1>(a, s, p, st);
-    else              backward<2>(a, s, p, st);
+    const BackPlan p = plan_back(a, lanes_of(a), static_cast<float*>(ws));
+    if (dt == 0)      backward<0>(a, p, st);
+    else if (dt == 1) backward<1>(a, p, st);
+    else              backward<2>(a, p, st);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (a.D % 4 == 0) k_headnorm_fold<4><<<a.B, kFoldThreads, 0, st>>>(a, p, accumulate, sqnorm);

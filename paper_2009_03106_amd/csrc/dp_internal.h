@@ -137,7 +137,7 @@ struct HeadnormArgs {
     const double* freqs;
     const int32_t* lengths;
 };
-constexpr int kMaxHeadDim = 1024;
+constexpr int kMaxHeadDim = 512;
 bool headnorm_fits(int64_t B, int64_t T, int64_t H0, int64_t H1);
 size_t headnorm_ws_bytes(int n_heads, int B, int T, int D);
 hipError_t launch_headnorm(const HeadnormArgs& a, int dt, hipStream_t st);

@@ -118,8 +118,8 @@ def full(heads):
 CASES = [  # B, T, heads, D, rot
     (1, 1, (1,), 1, 0), (1, 1, (1, 1), 2, 2), (2, 3, (4, 2), 7, 4), (1, 9, (3, 1), 8, 8), (3, 5, (5,), 16, 16), (2, 17, (6, 2), 20, 10),
     (1, 33, (2, 2), 33, 32), (2, 40, (12, 12), 64, 64), (1, 21, (8, 8), 80, 80), (2, 19, (3, 1), 96, 48), (5, 1, (32, 8), 128, 128),
-    (1, 300, (4, 4), 128, 64), (2, 13, (7, 1), 130, 66), (1, 37, (16, 2), 256, 256), (1, 5, (3,), 200, 200), (1, 7, (2, 1), 513, 512),
-    (1, 4, (2, 3), 1024, 1024), (1, 3, (1, 2), 1023, 6), (300, 2, (1, 1), 32, 32), (1, 2000, (1,), 64, 32), (3000, 1, (2, 1), 16, 16),
+    (1, 300, (4, 4), 128, 64), (2, 13, (7, 1), 130, 66), (1, 37, (16, 2), 256, 256), (1, 5, (3,), 200, 200), (1, 7, (2, 1), 511, 510),
+    (1, 4, (2, 3), 512, 512), (1, 3, (1, 2), 509, 6), (2, 9, (4, 1), 110, 110), (1, 33, (2, 5), 118, 38), (300, 2, (1, 1), 32, 32), (1, 2000, (1,), 64, 32), (3000, 1, (2, 1), 16, 16),
     (2, 31, (0, 3), 48, 16), (2, 11, (3, 0), 48, 32), (1, 4, (16, 16), 112, 112), (2, 70, (5, 3), 176, 96),
 ]
 
