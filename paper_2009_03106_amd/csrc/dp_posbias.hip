@@ -48,27 +48,54 @@ __global__ __launch_bounds__(kThreads) void k_posbias_add(PosbiasArgs a, const v
     const bool narrow = a.Tk < 8, last = k0 + 8 > a.Tk;
     const int over = (a.Tk + 7) / 8 * 8 - a.Tk;
     const int64_t in0 = b * a.s_b + h * a.s_h + (last && !narrow ? k0 - over : k0), out0 = b * a.o_b + h * a.o_h + k0;
+    // Four queries of this thread: step s is half a block of eight.
+    struct Step { int q0, nq, seen; };
+    const auto step_of = [&](int s) {
+        Step t;
+        t.q0 = (row0 + (s >> 1) * RG + rg) * 8 + 4 * (s & 1);
+        t.nq = s < 2 * tl.steps && nk > 0 ? min(4, w.nq - t.q0) : 0;
+        // the live keys of a query are its first ones: `seen` of the block's for the first query, one more for each other
+        t.seen = a.causal ? (int)min(max(t.q0 + w.start - k0 + 1, (int64_t)-8), (int64_t)8) : 8;
+        if (t.seen + 3 <= 0) t.nq = 0;
+        return t;
+    };
+    Raw8<DT> r[4];
+    const auto load = [&](const Step& t) {
+        const int64_t at = in0 + t.q0 * a.s_q;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < t.nq && !narrow) r[i] = load_raw8<DT>(scores, at + i * a.s_q);
+    };
+    Step t = step_of(0);
+    load(t);                                           // on their way while the biases are looked up
+    const auto bias_of = [&](int j) { return j >= 0 && j < a.n_buckets ? table[j * a.H + h] : 0.f; };
+    const float before = bias_of(a.buckets[0]), behind = bias_of(a.buckets[2 * a.reach]);      // of all distances beyond the reach
     const int distances = 8 * (CT + RG * tl.steps);
     for (int t0 = threadIdx.x; t0 < distances; t0 += 4 * kThreads) {
         int j[4];
         float v[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) j[i] = bucket_of(a, least + t0 + i * kThreads);
+        for (int i = 0; i < 4; ++i) {
+            const int64_t d = least + t0 + i * kThreads;
+            j[i] = d > -a.reach && d < a.reach ? a.buckets[d + a.reach] : -1;
+            v[i] = d <= -a.reach ? before : d >= a.reach ? behind : 0.f;
+        }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = j[i] >= 0 && j[i] < a.n_buckets ? table[j[i] * a.H + h] : 0.f;
+        for (int i = 0; i < 4; ++i)
+            if (j[i] >= 0 && j[i] < a.n_buckets) v[i] = table[j[i] * a.H + h];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (t0 + i * kThreads < distances) bias[t0 + i * kThreads] = v[i];
     }
     __syncthreads();
-    if (nk <= 0) return;
 #pragma unroll 1
     for (int s = 0; s < 2 * tl.steps; ++s) {
-        const int block = (s >> 1) * RG + rg, half = 4 * (s & 1), q0 = (row0 + block) * 8 + half, nq = min(4, w.nq - q0);
-        if (nq <= 0) break;
-        // the live keys of a query are its first ones: `seen` of the block's for the first query, one more for each other
-        const int seen = a.causal ? (int)min(max(q0 + w.start - k0 + 1, (int64_t)-8), (int64_t)8) : 8;
-        if (seen + 3 <= 0) continue;
+        if (s > 0) {
+            t = step_of(s);
+            load(t);
+        }
+        const int q0 = t.q0, nq = t.nq, seen = t.seen, block = (s >> 1) * RG + rg, half = 4 * (s & 1);
+        if (nq <= 0) continue;
         if (narrow) {
             for (int i = 0; i < nq; ++i)
                 for (int j = 0; j < min(nk, seen + i); ++j)
@@ -79,11 +106,6 @@ __global__ __launch_bounds__(kThreads) void k_posbias_add(PosbiasArgs a, const v
         const float4* cp = reinterpret_cast<const float4*>(bias + 8 * (ct + RG * tl.steps - 1 - block) + 4 - half);
 #pragma unroll
         for (int i = 0; i < 3; ++i) { const float4 f = cp[i]; c[4 * i] = f.x; c[4 * i + 1] = f.y; c[4 * i + 2] = f.z; c[4 * i + 3] = f.w; }
-        Raw8<DT> r[4];
-        const int64_t at = in0 + q0 * a.s_q;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < nq) r[i] = load_raw8<DT>(scores, at + i * a.s_q);
         const int64_t to = out0 + q0 * a.o_q;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {

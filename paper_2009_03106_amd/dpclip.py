@@ -819,20 +819,23 @@ def relative_buckets(n_buckets: int, reach: int, both: bool = True, device="cuda
     return torch.tensor(back[::-1] + ahead[1:], dtype=torch.int32, device=device)
 
 
+_ELEMENT_CODES = {torch.float32: DP_F32, torch.bfloat16: DP_BF16, torch.float16: DP_F16}
+
+
 def _inner(t: torch.Tensor, dims: int, name: str) -> int:
     """Address of a device tensor whose last dimension's elements are next to each other."""
-    if not t.is_cuda or t.dim() != dims or (t.shape[-1] > 1 and t.stride(-1) != 1):
+    if not t.is_cuda or t.dim() != dims or (t.stride(-1) != 1 and t.shape[-1] > 1):
         raise ValueError(f"{name} must be a device tensor of {dims} dimensions, the last one's elements next to each other")
-    if _dtype_code(t) > DP_F16:
+    if t.dtype not in _ELEMENT_CODES:
         raise TypeError(f"unsupported dtype {t.dtype}")
-    return t.data_ptr() if t.numel() > 0 else 0
+    return t.data_ptr()
 
 
 def _posbias_desc(x: torch.Tensor, out: Optional[torch.Tensor], buckets, n_buckets: int, q_start, q_lens, k_lens, causal) -> PosbiasDesc:
     B, H, Tq, Tk = x.shape
     s = x.stride()
     o = s if out is None else out.stride()
-    n = buckets.numel() if isinstance(buckets, torch.Tensor) else 0
+    n = buckets.numel()
     if n % 2 == 0:
         raise ValueError("buckets must hold one for each distance from -reach to reach")
     return PosbiasDesc(B, H, Tq, Tk, s[0], s[1], s[2], o[0], o[1], o[2], _vec(buckets, torch.int32, n, "buckets"), n // 2, int(n_buckets),
@@ -850,15 +853,18 @@ def posbias_add(scores: torch.Tensor, table: torch.Tensor, buckets: torch.Tensor
     Queries from q_lens[b] on, keys from k_lens[b] on and with causal the keys behind the query are left as they are in out."""
     lib = load_library()
     xp = _inner(scores, 4, "scores")
-    out = scores if out is None else out
-    op = _inner(out, 4, "out")
-    if out.shape != scores.shape or out.dtype != scores.dtype:
-        raise ValueError("out must have the shape and the dtype of scores")
+    if out is None:
+        out, op = scores, xp
+    else:
+        op = _inner(out, 4, "out")
+        if out.shape != scores.shape or out.dtype is not scores.dtype:
+            raise ValueError("out must have the shape and the dtype of scores")
     if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.shape[1] != scores.shape[1]:
         raise ValueError("table must be [n_buckets, H]")
     _here(stream, scores, out, table, buckets, q_start, q_lens, k_lens)
     d = _posbias_desc(scores, out, buckets, table.shape[0], q_start, q_lens, k_lens, causal)
-    st = lib.dp_posbias_add(ctypes.byref(d), xp, _f32(table, table.shape, "table"), _dtype_code(scores), op, _stream_ptr(stream))
+    st = lib.dp_posbias_add(ctypes.byref(d), xp, _vec(table, torch.float32, table.numel(), "table"), _ELEMENT_CODES[scores.dtype], op,
+                            _stream_ptr(stream))
     _check(st, "dp_posbias_add")
     return out
 
