@@ -156,28 +156,119 @@ struct Walk {
     int lc;                    // log2 of LC
     int R, C;                  // blocks of queries, of keys
     int m_first, bands;        // bands of LC diagonals of blocks, from m_first on
-    int segs;                  // pieces that a band's rows of blocks are cut into
     int wgs;                   // workgroups of an example's head; a group of lanes has one piece of one band
 };
+// rows of blocks in which band bd of an example has live elements: [lo, lo + the result)
+__device__ __forceinline__ int band_rows(const PosbiasArgs& a, const Walk& wk, const Window& w, int bd, int& lo) {
+    const int LC = 1 << wk.lc, m0 = wk.m_first + bd * LC;
+    lo = max(0, -(m0 + LC - 1));
+    return a.causal && (int64_t)8 * m0 - 7 > w.start ? 0 : max(0, min((w.nq + 7) / 8, (w.nk + 7) / 8 - m0) - lo);
+}
+// The pieces of all bands are numbered band by band: those of the first bands, with `before` rows together, end at this number.  Every
+// band has at least one, and of the others its share by rows.
+__host__ __device__ __forceinline__ int pieces_up_to(int bands, int64_t before, float share) { return bands + (int)((float)before * share); }
+__host__ __device__ __forceinline__ float share_of(int pieces, int bands, int64_t rows) { return rows > 0 ? (float)(pieces - bands) / (float)rows : 0.f; }
+// Piece number `task` of `tasks` (at least as many as bands): its band and rows [r0, r1).
+struct Piece { int band, r0, r1; };
+__device__ __forceinline__ Piece piece_of(const PosbiasArgs& a, const Walk& wk, const Window& w, int task, int tasks) {
+    int64_t all = 0;
+    int lo;
+    for (int bd = 0; bd < wk.bands; ++bd) all += band_rows(a, wk, w, bd, lo);
+    const float share = share_of(tasks, wk.bands, all);
+    int64_t before = 0;
+    int first = 0;
+    for (int bd = 0;; ++bd) {
+        const int rows = band_rows(a, wk, w, bd, lo);
+        before += rows;
+        const int next = bd + 1 == wk.bands ? tasks : pieces_up_to(bd + 1, before, share);
+        if (task < next) {
+            // (every piece's end is the next one's beginning by the same expression)
+            const int i = task - first, n = next - first;
+            const float step = (float)rows / (float)n;
+            return Piece{bd, lo + (int)((float)i * step), i + 1 == n ? lo + rows : lo + (int)((float)(i + 1) * step)};
+        }
+        first = next;
+    }
+}
 constexpr int kMaxSlots = kThreads * 8 + 8 * (kThreads / 8);
+
+// The groups' sums val [groups][8 LC + 8], slot 8 l + e of a group its diagonal 8 (m0 + l) + e - 7: the pieces of a band (next to each
+// other) are added into the first one's slots, then the slots by their buckets.
+__device__ __forceinline__ void fold_slots(const PosbiasArgs& a, const Walk& wk, int LC, double* val, short* bkt, const int* band_of, const Window& w,
+                                           int b, int h, double* __restrict__ partial, float* __restrict__ rows) {
+    const int tid = threadIdx.x, G = kThreads / LC, P = 8 * LC + 8;
+    __syncthreads();
+    // the first pieces of their bands here, as bits
+    const int lane = tid & (kWave - 1);
+    const uint64_t heads = __ballot(lane < G && (lane == 0 || band_of[lane] != band_of[max(lane - 1, 0)]));
+    for (uint64_t left = heads; left; left &= left - 1) {
+        const int from = __builtin_ctzll(left), to = left & (left - 1) ? __builtin_ctzll(left & (left - 1)) : G;
+        const int64_t nearest = (int64_t)8 * (wk.m_first + band_of[from] * LC) - 7 - w.start;
+        for (int x0 = tid; x0 < P; x0 += 4 * kThreads) {
+            int j[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {              // four look-ups at once
+                const int x = x0 + i * kThreads;
+                j[i] = x >= P || (a.causal && nearest + x > 0) ? -1 : bucket_of(a, nearest + x);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int x = x0 + i * kThreads;
+                if (x >= P) break;
+                double v = val[from * P + x];
+#pragma unroll 4
+                for (int t = from + 1; t < to; ++t) v += val[t * P + x];
+                val[from * P + x] = v;
+                bkt[from * P + x] = (short)(j[i] >= 0 && j[i] < a.n_buckets ? j[i] : -1);
+            }
+        }
+    }
+    __syncthreads();
+    // 2^ul threads for a bucket look through all slots
+    int ul = 6;
+    while (ul > 0 && (kThreads >> ul) < a.n_buckets) --ul;
+    const int u = tid & ((1 << ul) - 1);
+    for (int j0 = 0; j0 < a.n_buckets; j0 += kThreads >> ul) {
+        const int j = j0 + (tid >> ul);
+        double s = 0.0;
+        for (uint64_t left = heads; left; left &= left - 1) {
+            const int from = __builtin_ctzll(left) * P, to = from + P;
+            int k = from + u;
+            for (; k + (7 << ul) < to; k += 8 << ul) {
+                double v[8];
+                int c[8];
+#pragma unroll
+                for (int y = 0; y < 8; ++y) { v[y] = val[k + (y << ul)]; c[y] = bkt[k + (y << ul)]; }
+#pragma unroll
+                for (int y = 0; y < 8; ++y) s += c[y] == j ? v[y] : 0.0;
+            }
+            for (; k < to; k += 1 << ul) s += bkt[k] == j ? val[k] : 0.0;
+        }
+        for (int off = 1; off < 1 << ul; off <<= 1) s += __shfl_xor(s, off, kWave);
+        if (u == 0 && j < a.n_buckets) {
+            if (wk.wgs == 1) rows[((int64_t)b * a.n_buckets + j) * a.H + h] = (float)s;
+            else             partial[(int64_t)blockIdx.x * a.n_buckets + j] = s;
+        }
+    }
+}
 
 template <int DT>
 __global__ __launch_bounds__(kThreads, 3) void k_posbias_walk(PosbiasArgs a, const void* __restrict__ dS, Walk wk, double* __restrict__ partial, float* __restrict__ rows) {
     __shared__ double val[kMaxSlots];                  // [groups][8 LC + 8]: sums of the groups' diagonals
-    __shared__ double slot[kMaxSlots];                 // sums of the workgroup's diagonals
     __shared__ short bkt[kMaxSlots];                   // and their buckets
+    __shared__ int band_of[kThreads / 8];
     const int tid = threadIdx.x, LC = 1 << wk.lc, G = kThreads >> wk.lc, P = 8 * LC + 8;
     const int li = tid & (LC - 1), g = tid >> wk.lc;
     const int wg = blockIdx.x % wk.wgs, bh = blockIdx.x / wk.wgs, h = bh % a.H, b = bh / a.H;
     const Window w = window_of(a, b);
-    const int task = wg * G + g, band = task / wk.segs, seg = task - band * wk.segs;
-    const int m0 = wk.m_first + band * LC, m = m0 + li;
+    const Piece pc = piece_of(a, wk, w, wg * G + g, wk.wgs * G);
+    if (li == 0) band_of[g] = pc.band;
+    const int m0 = wk.m_first + pc.band * LC, m = m0 + li;
     double acc[15];
 #pragma unroll
     for (int e = 0; e < 15; ++e) acc[e] = 0.0;
-    if (band < wk.bands) {
-        const int lo = max(0, -(m0 + LC - 1)), hi = min(min(wk.R, (w.nq + 7) / 8), wk.C - m0), len = max(0, hi - lo);
-        const int r0 = lo + (int)((int64_t)len * seg / wk.segs), r1 = lo + (int)((int64_t)len * (seg + 1) / wk.segs);
+    {
+        const int r0 = pc.r0, r1 = pc.r1;
         const int64_t base = b * a.s_b + h * a.s_h;
         const bool narrow = a.Tk < 8;
         const int over = wk.C * 8 - a.Tk;              // how far the last block of keys reaches beyond the row
@@ -256,42 +347,7 @@ __global__ __launch_bounds__(kThreads, 3) void k_posbias_walk(PosbiasArgs a, con
         for (int y = 0; y < 7; ++y) v[8 + y] = acc[8 + y];
         v[15] = 0.0;
     }
-    // the pieces of a band are added: a slot per diagonal of each band that this workgroup has a piece of
-    const int t0 = wg * G, first = t0 / wk.segs, slots = (min(wk.bands - 1, (t0 + G - 1) / wk.segs) - first + 1) * P;
-    __syncthreads();
-    for (int s = tid; s < slots; s += kThreads) {
-        const int bd = first + s / P, x = s - (bd - first) * P, end = min((bd + 1) * wk.segs - t0, G);
-        double v = 0.0;
-        for (int t = max(bd * wk.segs - t0, 0); t < end; ++t) v += val[t * P + x];
-        slot[s] = v;
-        const int64_t distance = (int64_t)8 * (wk.m_first + bd * LC) + x - 7 - w.start;
-        const int j = a.causal && distance > 0 ? -1 : bucket_of(a, distance);
-        bkt[s] = (short)(j >= 0 && j < a.n_buckets ? j : -1);
-    }
-    __syncthreads();
-    // 2^ul threads for a bucket look through all slots
-    int ul = 6;
-    while (ul > 0 && (kThreads >> ul) < a.n_buckets) --ul;
-    const int u = tid & ((1 << ul) - 1);
-    for (int j0 = 0; j0 < a.n_buckets; j0 += kThreads >> ul) {
-        const int j = j0 + (tid >> ul);
-        double s = 0.0;
-        int k = u;
-        for (; k + (7 << ul) < slots; k += 8 << ul) {
-            double v[8];
-            int c[8];
-#pragma unroll
-            for (int y = 0; y < 8; ++y) { v[y] = slot[k + (y << ul)]; c[y] = bkt[k + (y << ul)]; }
-#pragma unroll
-            for (int y = 0; y < 8; ++y) s += c[y] == j ? v[y] : 0.0;
-        }
-        for (; k < slots; k += 1 << ul) s += bkt[k] == j ? slot[k] : 0.0;
-        for (int off = 1; off < 1 << ul; off <<= 1) s += __shfl_xor(s, off, kWave);
-        if (u == 0 && j < a.n_buckets) {
-            if (wk.wgs == 1) rows[((int64_t)b * a.n_buckets + j) * a.H + h] = (float)s;
-            else             partial[(int64_t)blockIdx.x * a.n_buckets + j] = s;
-        }
-    }
+    fold_slots(a, wk, LC, val, bkt, band_of, w, b, h, partial, rows);
 }
 
 // A workgroup per example: the sums of its heads' workgroups where there are several, and the squared norm of the rows.
@@ -331,9 +387,23 @@ __global__ __launch_bounds__(kFinishThreads) void k_posbias_finish(PosbiasArgs a
     sqnorm[b] = (float)(accumulate ? sqnorm[b] + sq : sq);
 }
 
-// How the blocks of a head are dealt.  Known keys behind every query (causal and no start of its own) get no bands.
-Walk plan_walk(int64_t BH, int Tq, int Tk, bool half) {
-    Walk w{};
+// How the blocks of a head are dealt.  Known keys behind every query (causal and no start of its own: half) get no bands.
+//
+// The workgroups of a head: the chip holds 768 at a time (three for each of the 256 compute units, by registers), and the loads of all
+// of them together are what bounds it, so that a launch takes as many rounds of 768 as it has, of a workgroup's longest piece and
+// about two steps for its fold.  The fewest steps so counted: 64 x 12 heads of 512 x 512 as 768 workgroups took 89 us, as 3072
+// 103 us.  Examples of their own lengths: two rounds at least, whose ends even out (4 x 16 heads of up to 4096 x 4096, causal: 121 us
+// in two rounds, 129 in three, 168 in five).
+constexpr int kAtATime = 768, kMostRounds = 8, kFoldSteps = 2;
+// rows of a band where everything is live
+int full_rows(const Walk& w, int bd) {
+    const int LC = 1 << w.lc, m0 = w.m_first + bd * LC;
+    return std::max(0, std::min(w.R, w.C - m0) - std::max(0, -(m0 + LC - 1)));
+}
+struct WalkPlan { Walk w; int64_t rows, least, most; };       // rows of all bands; workgroups of a head, at least and at most
+WalkPlan walk_of(int64_t BH, int Tq, int Tk, bool half) {
+    WalkPlan p{};
+    Walk& w = p.w;
     w.R = (Tq + 7) / 8;
     w.C = (Tk + 7) / 8;
     w.m_first = -(w.R - 1);
@@ -342,12 +412,40 @@ Walk plan_walk(int64_t BH, int Tq, int Tk, bool half) {
     while (w.lc < 5 && (1 << w.lc) < std::min(w.C, diagonals)) ++w.lc;
     const int LC = 1 << w.lc, G = kThreads / LC;
     w.bands = (diagonals + LC - 1) / LC;
-    // about eight workgroups for each of the 256 compute units, of pieces of at least four blocks
-    const int64_t want = std::max<int64_t>(1, std::min<int64_t>((2048 + BH - 1) / BH, ((int64_t)w.bands * ((w.R + 3) / 4) + G - 1) / G));
-    w.segs = (int)std::max<int64_t>(1, want * G / w.bands);
-    w.wgs = (int)(((int64_t)w.bands * w.segs + G - 1) / G);
-    return w;
+    for (int bd = 0; bd < w.bands; ++bd) p.rows += full_rows(w, bd);
+    p.least = (w.bands + G - 1) / G;
+    p.most = std::max(p.least, std::min(p.rows / (2 * G), kMostRounds * kAtATime / BH + 1));      // pieces of two steps at least
+    return p;
 }
+// rows of the longest piece
+int longest_piece(const Walk& w, int64_t all, int tasks) {
+    const float share = share_of(tasks, w.bands, all);
+    int64_t before = 0;
+    int first = 0, longest = 0;
+    for (int bd = 0; bd < w.bands; ++bd) {
+        const int rows = full_rows(w, bd);
+        before += rows;
+        const int next = bd + 1 == w.bands ? tasks : pieces_up_to(bd + 1, before, share);
+        longest = std::max(longest, (rows + next - first - 1) / (next - first));
+        first = next;
+    }
+    return longest;
+}
+Walk plan_walk(int64_t BH, int Tq, int Tk, bool half, bool ragged) {
+    WalkPlan p = walk_of(BH, Tq, Tk, half);
+    const int G = kThreads >> p.w.lc;
+    int64_t best = INT64_MAX;
+    for (int r = ragged ? 2 : 1; r <= kMostRounds; ++r) {
+        const int64_t k = std::max(p.least, std::min(p.most, r * kAtATime / BH));                 // the most that r rounds hold
+        const int64_t cost = ((k * BH + kAtATime - 1) / kAtATime) * (longest_piece(p.w, p.rows, (int)(k * G)) + kFoldSteps);
+        if (cost >= best) continue;
+        best = cost;
+        p.w.wgs = (int)k;
+    }
+    return p.w;
+}
+// the most workgroups of a head in any of the plans
+int64_t most_wgs(int64_t BH, int Tq, int Tk) { return std::max(walk_of(BH, Tq, Tk, false).most, walk_of(BH, Tq, Tk, true).most); }
 
 }  // namespace
 
@@ -358,12 +456,12 @@ bool posbias_fits(int64_t B, int64_t H, int64_t Tq, int64_t Tk) {
     if (H > most / B || Tq > most / (B * H)) return false;
     const AddTiles t = plan_add(B * H, (int)Tq, (int)Tk);
     return launch_holds(B * H * t.row_tiles * t.col_tiles, kThreads)
-        && B < 1 << 22 && launch_holds(B * H * plan_walk(B * H, (int)Tq, (int)Tk, false).wgs, kThreads) && launch_holds(B * H * plan_walk(B * H, (int)Tq, (int)Tk, true).wgs, kThreads);
+        && B < 1 << 22 && launch_holds(B * H * most_wgs(B * H, (int)Tq, (int)Tk), kThreads);
 }
 // the sums of every workgroup, where a head has several; whether keys are left out is not known here
 size_t posbias_ws_bytes(int B, int H, int Tq, int Tk) {
     const int64_t BH = (int64_t)B * H;
-    const int wgs = std::max(plan_walk(BH, Tq, Tk, false).wgs, plan_walk(BH, Tq, Tk, true).wgs);
+    const int64_t wgs = most_wgs(BH, Tq, Tk);
     return wgs > 1 ? (size_t)BH * wgs * kMaxBuckets * sizeof(double) : 16;
 }
 
@@ -378,7 +476,7 @@ hipError_t launch_posbias_add(const PosbiasArgs& a, const void* scores, const fl
 
 hipError_t launch_posbias_sqnorm(const PosbiasArgs& a, const void* dS, int dt, bool accumulate, float* rows, float* sqnorm, void* ws, hipStream_t st) {
     const int64_t BH = (int64_t)a.B * a.H;
-    const Walk w = plan_walk(BH, a.Tq, a.Tk, a.causal && !a.q_start);
+    const Walk w = plan_walk(BH, a.Tq, a.Tk, a.causal && !a.q_start, a.q_lens || a.k_lens);
     const unsigned grid = (unsigned)(BH * w.wgs);
     double* partial = static_cast<double*>(ws);
     if (dt == 0)      k_posbias_walk<0><<<grid, kThreads, 0, st>>>(a, dS, w, partial, rows);
