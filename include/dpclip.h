@@ -459,7 +459,7 @@ size_t dp_tensors_workspace_bytes(int64_t n_tensors);
  * pair (q, k) is live if q < q_lens[b], k < k_lens[b] and, with `causal`, k <= q +
  * q_start[b]; what is not live counts for nothing and is not written, whatever is there. */
 typedef struct {
-    int64_t B, H, Tq, Tk;
+    int64_t B, H, Tq, Tk;      /* Tq and Tk at most 2^20 */
     int64_t s_b, s_h, s_q;     /* strides of the scores (or dS) in elements, >= 0; keys are next to each other */
     int64_t o_b, o_h, o_q;     /* strides of dp_posbias_add's output */
     const int32_t* buckets;    /* device, [2 reach + 1]: the bucket of each distance from -reach to reach; distances beyond

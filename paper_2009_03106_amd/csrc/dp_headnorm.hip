@@ -162,12 +162,12 @@ __device__ __forceinline__ float row_sum(float v, int L) {
 }
 
 struct Token { int b, t, position; bool live; };
-__device__ __forceinline__ Token token_of(const HeadnormArgs& a, int64_t n) {
+__device__ __forceinline__ Token token_of(const HeadnormArgs& a, int n) {      // fewer than 2^30
     Token k;
-    k.live = n < (int64_t)a.B * a.T;
-    const int64_t at = k.live ? n : 0;
-    k.b = (int)(at / a.T);
-    k.t = (int)(at - (int64_t)k.b * a.T);
+    k.live = n < a.B * a.T;
+    const int at = k.live ? n : 0;
+    k.b = at / a.T;
+    k.t = at - k.b * a.T;
     if (a.lengths) k.live = k.live && k.t < a.lengths[k.b];
     k.position = a.positions ? a.positions[k.b * a.positions_b + k.t] : k.t;
     return k;
@@ -183,8 +183,8 @@ __global__ __launch_bounds__(kThreads) void k_headnorm(HeadnormArgs a, Rows w) {
     const int it0 = (int)((int64_t)w.its * part / w.split), it1 = (int)((int64_t)w.its * (part + 1) / w.split);
     const Pieces pc = pieces<PAIRS, WHOLE>(a, l);
     const float mean = 1.0f / a.D;
-    for (int64_t n0 = wave / w.split * w.tw; n0 < (int64_t)a.B * a.T; n0 += step * w.tw) {
-        const Token k = token_of(a, n0 + g / w.hw);
+    for (int64_t n0 = wave / w.split * w.tw; n0 < a.B * a.T; n0 += step * w.tw) {
+        const Token k = token_of(a, (int)n0 + g / w.hw);
         Turn turn;
         turn.of(a, k.position, l, k.live);
 #pragma unroll 1
@@ -451,7 +451,7 @@ template <int DT> void backward(const HeadnormArgs& a, const BackPlan& p, hipStr
 
 bool headnorm_fits(int64_t B, int64_t T, int64_t H0, int64_t H1) {
     const int64_t most = int64_t(1) << 30;
-    if (B > (int64_t(1) << 22) || T > most || H0 > most || H1 > most) return false;
+    if (!launch_holds(B, kFoldThreads) || T > most || H0 > most || H1 > most) return false;
     return B == 0 || T <= most / B;
 }
 size_t headnorm_ws_bytes(int n_heads, int B, int T, int D) { return (size_t)B * most_chunks(B, T) * n_heads * D * sizeof(float); }

@@ -122,6 +122,7 @@ struct PosbiasArgs {
     int causal;
 };
 constexpr int kMaxBuckets = 1024;
+constexpr int64_t kMaxLength = int64_t(1) << 20;       // queries, keys
 bool posbias_fits(int64_t B, int64_t H, int64_t Tq, int64_t Tk);       // what the launches below hold
 size_t posbias_ws_bytes(int B, int H, int Tq, int Tk);
 hipError_t launch_posbias_add(const PosbiasArgs& a, const void* scores, const float* table, int dt, void* out, hipStream_t st);

@@ -451,12 +451,12 @@ int64_t most_wgs(int64_t BH, int Tq, int Tk) { return std::max(walk_of(BH, Tq, T
 
 bool posbias_fits(int64_t B, int64_t H, int64_t Tq, int64_t Tk) {
     const int64_t most = int64_t(1) << 31;
-    if (B >= most || H >= most || Tq >= most / 2 || Tk >= most / 2) return false;
+    if (B >= most || H >= most || Tq > kMaxLength || Tk > kMaxLength) return false;
     if (B == 0 || H == 0 || Tq == 0 || Tk == 0) return true;
     if (H > most / B || Tq > most / (B * H)) return false;
     const AddTiles t = plan_add(B * H, (int)Tq, (int)Tk);
     return launch_holds(B * H * t.row_tiles * t.col_tiles, kThreads)
-        && B < 1 << 22 && launch_holds(B * H * most_wgs(B * H, (int)Tq, (int)Tk), kThreads);
+        && launch_holds(B, kFinishThreads) && launch_holds(B * H * most_wgs(B * H, (int)Tq, (int)Tk), kThreads);
 }
 // the sums of every workgroup, where a head has several; whether keys are left out is not known here
 size_t posbias_ws_bytes(int B, int H, int Tq, int Tk) {

@@ -663,6 +663,11 @@ def _here(stream: Optional[torch.cuda.Stream], *tensors) -> int:
     return dev
 
 
+def _queue(stream: Optional[torch.cuda.Stream], dev: int) -> int:
+    """_stream_ptr for a device index that is known already."""
+    return int(stream.cuda_stream) if stream is not None else int(_raw_stream(dev)) if _raw_stream is not None else _stream_ptr(None)
+
+
 def _vec(t: Optional[torch.Tensor], dtype: torch.dtype, n: int, name: str) -> Optional[int]:
     """Address of a contiguous tensor of n elements (on the current device: _here)."""
     if t is None:
@@ -743,14 +748,14 @@ def tensors_norm(tensors, norm: Optional[torch.Tensor] = None, *, accumulate: bo
     n = len(descs.arr)
     if norm is None and accumulate:
         raise ValueError("accumulate needs an existing norm tensor")
-    _here(stream, norm, tensor_norms, workspace)
+    dev = _here(stream, norm, tensor_norms, workspace)
     descs.here()
     with _made_on(stream):
         if norm is None:
             norm = torch.empty(1, dtype=torch.float32, device=descs.device)
         ws = _workspace(lambda: tensors_workspace_bytes(descs), descs.device, workspace)
     st = lib.dp_tensors_norm(descs.arr, n, int(bool(accumulate)), _f32(norm, (1,), "norm"), _f32(tensor_norms, (n,), "tensor_norms"),
-                             *_ws_args(ws), _stream_ptr(stream))
+                             *_ws_args(ws), _queue(stream, dev))
     _check(st, "dp_tensors_norm")
     return norm
 
@@ -765,12 +770,12 @@ def tensors_clip(tensors, norm: torch.Tensor, C: float, outs=None, *, accumulate
         if accumulate and outs is None:
             raise ValueError("accumulate needs existing outs")
         descs = tensor_descs(tensors, outs, in_place=outs is None)
-    _here(stream, norm, workspace)
+    dev = _here(stream, norm, workspace)
     descs.here()
     with _made_on(stream):
         ws = _workspace(lambda: tensors_workspace_bytes(descs), descs.device, workspace)
     st = lib.dp_tensors_clip(descs.arr, len(descs.arr), _f32(norm, (1,), "norm"), float(C), int(bool(accumulate)),
-                             *_ws_args(ws), _stream_ptr(stream))
+                             *_ws_args(ws), _queue(stream, dev))
     _check(st, "dp_tensors_clip")
     return descs.outs
 
@@ -786,14 +791,14 @@ def tensors_norm_clip(tensors, C: float, outs=None, *, accumulate: bool = False,
             raise ValueError("accumulate needs existing outs")
         descs = tensor_descs(tensors, outs, in_place=outs is None)
     n = len(descs.arr)
-    _here(stream, norm, tensor_norms, workspace)
+    dev = _here(stream, norm, tensor_norms, workspace)
     descs.here()
     with _made_on(stream):
         if norm is None:
             norm = torch.empty(1, dtype=torch.float32, device=descs.device)
         ws = _workspace(lambda: tensors_workspace_bytes(descs), descs.device, workspace)
     st = lib.dp_tensors_norm_clip(descs.arr, n, float(C), int(bool(accumulate)), _f32(norm, (1,), "norm"),
-                                  _f32(tensor_norms, (n,), "tensor_norms"), *_ws_args(ws), _stream_ptr(stream))
+                                  _f32(tensor_norms, (n,), "tensor_norms"), *_ws_args(ws), _queue(stream, dev))
     _check(st, "dp_tensors_norm_clip")
     return norm
 
@@ -861,10 +866,10 @@ def posbias_add(scores: torch.Tensor, table: torch.Tensor, buckets: torch.Tensor
             raise ValueError("out must have the shape and the dtype of scores")
     if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.shape[1] != scores.shape[1]:
         raise ValueError("table must be [n_buckets, H]")
-    _here(stream, scores, out, table, buckets, q_start, q_lens, k_lens)
+    dev = _here(stream, scores, out, table, buckets, q_start, q_lens, k_lens)
     d = _posbias_desc(scores, out, buckets, table.shape[0], q_start, q_lens, k_lens, causal)
     st = lib.dp_posbias_add(ctypes.byref(d), xp, _vec(table, torch.float32, table.numel(), "table"), _ELEMENT_CODES[scores.dtype], op,
-                            _stream_ptr(stream))
+                            _queue(stream, dev))
     _check(st, "dp_posbias_add")
     return out
 
@@ -885,7 +890,7 @@ def posbias_sqnorm(dS: torch.Tensor, buckets: torch.Tensor, n_buckets: int, sqno
     B, H = dS.shape[0], dS.shape[1]
     if sqnorm is None and accumulate:
         raise ValueError("accumulate needs an existing sqnorm tensor")
-    _here(stream, dS, sqnorm, rows, buckets, q_start, q_lens, k_lens, workspace)
+    dev = _here(stream, dS, sqnorm, rows, buckets, q_start, q_lens, k_lens, workspace)
     d = _posbias_desc(dS, None, buckets, n_buckets, q_start, q_lens, k_lens, causal)
     with _made_on(stream):
         if sqnorm is None:
@@ -894,7 +899,7 @@ def posbias_sqnorm(dS: torch.Tensor, buckets: torch.Tensor, n_buckets: int, sqno
             rows = torch.empty((B, n_buckets, H), dtype=torch.float32, device=dS.device)
         ws = _workspace(lambda: posbias_workspace_bytes(dS), dS.device, workspace)
     st = lib.dp_posbias_sqnorm(ctypes.byref(d), xp, _dtype_code(dS), int(bool(accumulate)), _f32(sqnorm, (B,), "sqnorm"),
-                               _f32(rows, (B, n_buckets, H), "rows"), *_ws_args(ws), _stream_ptr(stream))
+                               _f32(rows, (B, n_buckets, H), "rows"), *_ws_args(ws), _queue(stream, dev))
     _check(st, "dp_posbias_sqnorm")
     return sqnorm, rows
 
@@ -983,10 +988,10 @@ def headnorm(heads, outs=None, *, freqs: Optional[torch.Tensor] = None, position
                 make = torch.empty if lengths is None else torch.zeros
                 outs = [make(x.shape, dtype=x.dtype, device=x.device) for x, _ in heads]
         descs = head_descs(heads, outs)
-    _here(stream, freqs, positions, lengths)
+    dev = _here(stream, freqs, positions, lengths)
     descs.here()
     d = _headnorm_desc(descs, freqs, positions, lengths, pairs, eps)
-    st = lib.dp_headnorm(ctypes.byref(d), descs.arr, len(descs.arr), descs.dtype, _stream_ptr(stream))
+    st = lib.dp_headnorm(ctypes.byref(d), descs.arr, len(descs.arr), descs.dtype, _queue(stream, dev))
     _check(st, "dp_headnorm")
     return descs.outs
 
@@ -1020,11 +1025,11 @@ def headnorm_sqnorm(heads, dys, sqnorm: Optional[torch.Tensor] = None, outs=None
         if sqnorm is None:
             sqnorm = torch.empty(descs.B, dtype=torch.float32, device=descs.device)
         ws = _workspace(lambda: headnorm_workspace_bytes(descs), descs.device, workspace)
-    _here(stream, sqnorm, freqs, positions, lengths, workspace)
+    dev = _here(stream, sqnorm, freqs, positions, lengths, workspace)
     descs.here()
     d = _headnorm_desc(descs, freqs, positions, lengths, pairs, eps)
     st = lib.dp_headnorm_sqnorm(ctypes.byref(d), descs.arr, len(descs.arr), descs.dtype, int(bool(accumulate)),
-                                _f32(sqnorm, (descs.B,), "sqnorm"), *_ws_args(ws), _stream_ptr(stream))
+                                _f32(sqnorm, (descs.B,), "sqnorm"), *_ws_args(ws), _queue(stream, dev))
     _check(st, "dp_headnorm_sqnorm")
     return sqnorm, descs.gain_rows, descs.outs
 

@@ -167,6 +167,32 @@ def test_graph_replays_and_streams():
     assert torch.equal(got, norm)
 
 
+def test_long_lists_in_graphs_and_calls_at_once():
+    """More tensors than a launch's arguments hold, captured; two lists on two streams at the same time."""
+    lists = [make([100 + 7 * i for i in range(150)], [F32, BF16, F16] * 50, seed=s) for s in (1, 2)]
+    outs = [[torch.empty_like(x) for x in xs] for xs in lists]
+    descs = [dp.tensor_descs(xs, os) for xs, os in zip(lists, outs)]
+    norms = [torch.empty(1, device="cuda") for _ in lists]
+    ws = [torch.empty(dp.tensors_workspace_bytes(d), dtype=torch.uint8, device="cuda") for d in descs]
+    streams = [torch.cuda.Stream() for _ in lists]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for i, st in enumerate(streams):
+            dp.tensors_norm_clip(None, 1.0, norm=norms[i], descs=descs[i], workspace=ws[i], stream=st)
+    torch.cuda.synchronize()
+    for i in range(2):
+        check(lists[i], outs[i], norms[i], 1.0)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        dp.tensors_norm_clip(None, 1.0, norm=norms[0], descs=descs[0], workspace=ws[0])
+    for k in range(3):
+        for x in lists[0]:
+            x.mul_(0.5)
+        g.replay()
+        torch.cuda.synchronize()
+        check(lists[0], outs[0], norms[0], 1.0)
+
+
 def test_results_repeat():
     xs = make([1_000_003, 12345, 8], [F32, BF16, F16], seed=6)
     first = [t.clone() for t in (dp.tensors_norm_clip(xs, 1.0, [torch.empty_like(x) for x in xs]),)]

@@ -40,6 +40,8 @@ def test_gradient_refusals(lib):
     assert grad(lib, s_b=0, s_h=0, s_q=0) == dp.DP_ERR_WORKSPACE                 # broadcast gradients
     assert grad(lib, s_b=1 << 49) == dp.DP_ERR_UNSUPPORTED
     assert grad(lib, B=1 << 31) == dp.DP_ERR_UNSUPPORTED
+    for name in ("Tq", "Tk"):
+        assert grad(lib, **{name: 1 << 20}) == dp.DP_ERR_WORKSPACE and grad(lib, **{name: (1 << 20) + 1}) == dp.DP_ERR_UNSUPPORTED
     assert grad(lib, B=1 << 20, H=1 << 20) == dp.DP_ERR_UNSUPPORTED
     assert lib.dp_posbias_sqnorm(None, A, dp.DP_F32, 0, A, A, None, 0, None) == dp.DP_ERR_INVALID_ARG
     need = lib.dp_posbias_workspace_bytes(2, 3, 5, 7)
