@@ -401,33 +401,52 @@ Rows rows_of(int H0, int H1, int L, int turns) {
     return w;
 }
 
-// The most chunks that an example's tokens are cut into in the backward pass: 1536 workgroups in all (twice what the 256 compute
-// units have registers for at a time), and no more than the fold adds up in a few microseconds.
-constexpr int kBackGroups = 1536, kBackChunks = 512;
-int most_chunks(int B, int T) { return std::max(1, std::min({kBackChunks, T, kBackGroups / B})); }
+// Chunks of an example's tokens in the backward pass.  The chip holds 768 workgroups at a time (three for each of the 256 compute
+// units by registers, four for some types), and a launch takes about as many rounds of 768 as it has, of the steps of a wave (a row
+// for each of its groups of lanes) and about four more for its beginning and its end.  29 examples of up to 7231 tokens of 5 + 1
+// heads of 64 bf16: 94 us so, 107 us in rounds of 1024, 98 us in 1536 workgroups whatever the sizes.
+constexpr int kAtATime = 768, kMostRounds = 6, kBackChunks = 512, kEndSteps = 4;
+int most_chunks(int B, int T) { return std::max(1, std::min({kBackChunks, T, kMostRounds * kAtATime / B})); }
 
-// Descriptors with more heads get shorter chunks, so that all workgroups have about the same number of rows.  Where waves are few,
-// two or four of a workgroup share a token's heads.
-BackPlan plan_back(const HeadnormArgs& a, int L, float* partial) {
-    BackPlan p{};
-    const int waves = kThreads / kWave, most = most_chunks(a.B, a.T);
-    int64_t steps = 0;                                  // of all waves together
-    for (int i = 0; i < a.n_heads; ++i) {
-        Rows& w = p.of[i].w;
-        w = rows_of(a.heads[i].H, 0, L, kTurns);
-        steps += (int64_t)a.B * ceil_div(a.T, w.tw) * w.its;
-    }
-    const int64_t per_wave = std::max<int64_t>(1, steps / (kBackGroups * waves));
+// A wave gets about per_wave steps: descriptors with more heads get shorter chunks; where tokens are few, two or four waves of a
+// workgroup share their heads.
+struct BackCost { int64_t workgroups; int steps; };
+BackCost cut_back(const HeadnormArgs& a, int64_t per_wave, BackPlan& p) {
+    constexpr int waves = kThreads / kWave;
+    const int most = most_chunks(a.B, a.T);
+    BackCost c{};
     for (int i = 0; i < a.n_heads; ++i) {
         Back& k = p.of[i];
+        k.w.split = 1;
         while (k.w.split < waves && k.w.split * 2 <= k.w.its && k.w.its / k.w.split > per_wave) k.w.split *= 2;
-        const int granule = waves / k.w.split * k.w.tw; // tokens that a workgroup has at a time
-        const int64_t rounds = std::max<int64_t>(1, per_wave * k.w.split / std::max(1, k.w.its));
-        k.tokens = (int)std::min<int64_t>(a.T, granule * std::max<int64_t>(rounds, ceil_div(ceil_div(a.T, granule), most)));
+        const int granule = waves / k.w.split * k.w.tw, its = ceil_div(std::max(1, k.w.its), k.w.split);      // tokens that a workgroup has at a time, steps for them
+        const int64_t rounds = std::max<int64_t>({1, per_wave / its, ceil_div(ceil_div(a.T, granule), most)});
+        k.tokens = (int)std::min<int64_t>(a.T, granule * rounds);
         k.chunks = ceil_div(a.T, k.tokens);
-        k.partial = partial;
-        partial += (int64_t)a.B * most * a.D;
+        c.workgroups += (int64_t)a.B * k.chunks;
+        c.steps = std::max<int>(c.steps, ceil_div(k.tokens, granule) * its);
     }
+    return c;
+}
+BackPlan plan_back(const HeadnormArgs& a, int L, float* partial) {
+    BackPlan p{};
+    int64_t steps = 0;                                  // of all waves together
+    for (int i = 0; i < a.n_heads; ++i) {
+        p.of[i].w = rows_of(a.heads[i].H, 0, L, kTurns);
+        p.of[i].partial = partial + (int64_t)i * a.B * most_chunks(a.B, a.T) * a.D;
+        steps += (int64_t)a.B * ceil_div(a.T, p.of[i].w.tw) * p.of[i].w.its;
+    }
+    int64_t best = INT64_MAX, best_per_wave = 1;
+    for (int r = a.lengths ? 2 : 1; r <= kMostRounds; ++r) {            // (lengths: the ends of at least two rounds even out)
+        constexpr int waves = kThreads / kWave;
+        const int64_t per_wave = std::max<int64_t>(1, (steps + kAtATime * waves * r - 1) / (kAtATime * waves * r));
+        const BackCost c = cut_back(a, per_wave, p);
+        const int64_t cost = (c.workgroups + kAtATime - 1) / kAtATime * (c.steps + kEndSteps);
+        if (cost >= best) continue;
+        best = cost;
+        best_per_wave = per_wave;
+    }
+    cut_back(a, best_per_wave, p);
     p.first = a.B * p.of[0].chunks;
     return p;
 }
