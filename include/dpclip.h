@@ -459,14 +459,14 @@ size_t dp_tensors_workspace_bytes(int64_t n_tensors);
  * pair (q, k) is live if q < q_lens[b], k < k_lens[b] and, with `causal`, k <= q +
  * q_start[b]; what is not live counts for nothing and is not written, whatever is there. */
 typedef struct {
-    int64_t B, H, Tq, Tk;      /* Tq and Tk at most 2^20 */
+    int64_t B, H, Tq, Tk;      /* Tq and Tk at most 2^20; fewer than 2^22 examples */
     int64_t s_b, s_h, s_q;     /* strides of the scores (or dS) in elements, >= 0; keys are next to each other */
     int64_t o_b, o_h, o_q;     /* strides of dp_posbias_add's output */
     const int32_t* buckets;    /* device, [2 reach + 1]: the bucket of each distance from -reach to reach; distances beyond
                                   have the first or the last one's.  A bucket outside [0, n_buckets) adds nothing and gets
                                   no gradient */
     int64_t reach;             /* 0 to 2^20 */
-    int64_t n_buckets;         /* 1 to 1024 */
+    int64_t n_buckets;         /* 1 to 1024; n_buckets H at most 2^30 */
     const int32_t* q_start;    /* NULL: 0 for all; or device int32[B] */
     const int32_t* q_lens;     /* NULL: Tq for all; or device int32[B], taken as 0 below 0 and as Tq above Tq */
     const int32_t* k_lens;     /* NULL: Tk for all; or device int32[B], likewise */
@@ -475,12 +475,14 @@ typedef struct {
 
 /* out = scores + bias.  scores and out: device, `dtype` (DP_F32, DP_BF16 or DP_F16; 8-bit types give
  * DP_ERR_UNSUPPORTED), aligned to one element; the sum is taken in float32 and rounded once.  out may be scores with
- * the same strides; otherwise no element of out is one of scores, and no two elements of out share one.   table: device float32[n_buckets, H] */
+ * the same strides; otherwise no element of out is one of scores, and no two elements of out share one.
+ *   table      device float32[n_buckets, H] */
 dp_status dp_posbias_add(const dp_posbias_desc* desc, const void* scores, const float* table, dp_dtype dtype,
                          void* out, void* hip_stream);
 
 /* rows as above, and sqnorm[b] = (accumulate ? sqnorm[b] : 0) + ||rows[b]||^2.  The clipped sum of the rows is
- * dp_clipped_bias_grad(rows, clip, B, n_buckets * H, ...).  The sums of the diagonals and buckets are taken in 64 bits.
+ * dp_clipped_bias_grad(rows, clip, B, n_buckets * H, ...).  Up to eight neighbours
+ * of a diagonal are added in float32, everything else in 64 bits.
  *   dS         device, `dtype`, aligned to one element; the strides o_* are not looked at
  *   rows       device float32[B, n_buckets, H], written
  *   sqnorm     device float32[B]
@@ -508,18 +510,18 @@ typedef struct {
     const void* x;             /* device, `dtype`, aligned to one element: [B, T, H, D] with the strides below (in elements,
                                   >= 0), the D numbers of a row next to each other; read only unless out is x */
     int64_t x_b, x_t, x_h;
-    int64_t H;                 /* heads (queries and keys may have different numbers) */
+    int64_t H;                 /* heads, at most 2^20 (queries and keys may have different numbers) */
     const float* gain;         /* device float32[D] */
     void* out;                 /* device, `dtype`: y, or dx.  May be x (or dy) itself with the same strides; no other element of
                                   any out of the call is an element of an input or of another out */
     int64_t o_b, o_t, o_h;
     const void* dy;            /* dp_headnorm_sqnorm only: the gradient of y */
     int64_t dy_b, dy_t, dy_h;
-    float* gain_rows;          /* dp_headnorm_sqnorm only: device float32[B, D], written */
+    float* gain_rows;          /* dp_headnorm_sqnorm only: device float32[B, D], written; rows of its own for each descriptor */
 } dp_heads_desc;
 
 typedef struct {
-    int64_t B, T, D;           /* D at most 512 */
+    int64_t B, T, D;           /* D at most 512, fewer than 2^22 examples, B T at most 2^30 */
     int64_t rot;               /* even, 0 to D */
     dp_rotation rotation;
     float eps;                 /* > 0 */

@@ -62,6 +62,11 @@ dp_status check(const dp_headnorm_desc* desc, const dp_heads_desc* heads, int64_
             if (k > i && !tensors_apart(out, strided(d, g, g.out, g.o_b, g.o_t, g.o_h, es))) return DP_ERR_INVALID_ARG;
         }
     }
+    // one gain for both: each descriptor's rows are written by themselves, so they need rows of their own
+    if (backward && n_heads > 1 && heads[0].gain_rows && heads[1].gain_rows) {
+        const Strided r0{heads[0].gain_rows, {1, 1, 1}, {0, 0, 0}, d.B * d.D, 4}, r1{heads[1].gain_rows, {1, 1, 1}, {0, 0, 0}, d.B * d.D, 4};
+        if (!tensors_apart(r0, r1)) return DP_ERR_INVALID_ARG;
+    }
     return DP_OK;
 }
 

@@ -7,6 +7,7 @@ using namespace dpk;
 namespace {
 
 constexpr int64_t kMaxReach = int64_t(1) << 20;
+constexpr int64_t kMaxTable = int64_t(1) << 30;        // its elements have int offsets in the kernels
 
 bool element_aligned(const void* p, dp_dtype d) { return reinterpret_cast<uintptr_t>(p) % (d == DP_F32 ? 4 : 2) == 0; }
 
@@ -16,6 +17,7 @@ dp_status check(const dp_posbias_desc* d, dp_dtype dtype) {
     if (dtype != DP_F32 && dtype != DP_BF16 && dtype != DP_F16) return DP_ERR_INVALID_ARG;
     if (d->s_b < 0 || d->s_h < 0 || d->s_q < 0) return DP_ERR_INVALID_ARG;
     if (d->reach > kMaxReach || d->n_buckets > kMaxBuckets || !posbias_fits(d->B, d->H, d->Tq, d->Tk)) return DP_ERR_UNSUPPORTED;
+    if (d->n_buckets * d->H > kMaxTable) return DP_ERR_UNSUPPORTED;
     if (too_far(d->B, d->s_b) || too_far(d->H, d->s_h) || too_far(d->Tq, d->s_q)) return DP_ERR_UNSUPPORTED;
     return DP_OK;
 }
@@ -66,7 +68,6 @@ dp_status dp_posbias_sqnorm(const dp_posbias_desc* desc, const void* dS, dp_dtyp
         return DP_OK;
     }
     if (!dS || !rows || !d.buckets || !element_aligned(dS, dtype)) return DP_ERR_INVALID_ARG;
-    if (width > INT32_MAX) return DP_ERR_UNSUPPORTED;
     if (!workspace || workspace_bytes < posbias_ws_bytes((int)d.B, (int)d.H, (int)d.Tq, (int)d.Tk) || ((uintptr_t)workspace & 15) != 0) return DP_ERR_WORKSPACE;
     const hipError_t e = launch_posbias_sqnorm(args_of(d), dS, (int)dtype, accumulate != 0, rows, sqnorm, workspace, st);
     return e == hipSuccess ? DP_OK : DP_ERR_HIP;

@@ -469,9 +469,9 @@ template <int DT> void backward(const HeadnormArgs& a, const BackPlan& p, hipStr
 }  // namespace
 
 bool headnorm_fits(int64_t B, int64_t T, int64_t H0, int64_t H1) {
-    const int64_t most = int64_t(1) << 30;
-    if (!launch_holds(B, kFoldThreads) || T > most || H0 > most || H1 > most) return false;
-    return B == 0 || T <= most / B;
+    const int64_t tokens = int64_t(1) << 30, heads = int64_t(1) << 20;
+    if (!launch_holds(B, kFoldThreads) || T > tokens || H0 > heads || H1 > heads) return false;
+    return B == 0 || T <= tokens / B;
 }
 size_t headnorm_ws_bytes(int n_heads, int B, int T, int D) { return (size_t)B * most_chunks(B, T) * n_heads * D * sizeof(float); }
 

@@ -150,8 +150,8 @@ AddTiles plan_add(int64_t BH, int Tq, int Tk) {
 // All of them have their elements on the same 15 diagonals, k - q = 8 m + e with -7 <= e <= 7, so the sums stay in the lane's
 // registers, and a group of LC lanes with neighbouring m reads LC pieces of 16 bytes (8 of float32: 32) next to each other
 // of every query.  The diagonal of a block is added in float32 (at most 8 elements), the blocks in 64 bits.
-// A thread per diagonal, one element after the other in 64 bits, took 2950 us for 64 x 12 x 512 x 512 bf16; see the table of
-// measurements at launch_posbias_rows.
+// 64 x 12 x 512 x 512 bf16: 88 us (4.6 TB/s; a copy of 4 GiB reaches 4.8).  A thread per diagonal, one element after the other in 64
+// bits, took 2950 us.
 struct Walk {
     int lc;                    // log2 of LC
     int R, C;                  // blocks of queries, of keys

@@ -966,8 +966,10 @@ def _headnorm_desc(d: HeadDescs, freqs, positions, lengths, pairs, eps) -> Headn
         rot = 2 * freqs.numel()
     pp, pb = None, 0
     if positions is not None:
+        if positions.shape not in ((d.T,), (d.B, d.T)):
+            raise ValueError(f"positions must be [{d.T}] or [{d.B}, {d.T}], got {tuple(positions.shape)}")
         pb = d.T if positions.dim() == 2 else 0
-        pp = _vec(positions, torch.int32, d.B * d.T if positions.dim() == 2 else d.T, "positions")
+        pp = _vec(positions, torch.int32, positions.numel(), "positions")
     return HeadnormDesc(d.B, d.T, d.D, rot, int(bool(pairs)), float(eps), pp, pb, freqs.data_ptr() if rot else None,
                         _vec(lengths, torch.int32, d.B, "lengths"))
 

@@ -7,8 +7,8 @@ Tolerances, in half steps of float32 (2^-24), from the chains of float32 operati
      magnitudes of the pair before the turn; one rounding to the type behind it.
   u: 4 + 2 of |dy_a| + |dy_b| =: U.   x r: 17.   mean(u w x r): 6 + 1 + 17 + 1 of each term and 23 for the sum: 48 of the mean of
      magnitudes M.   dx = r (u w - x r mean): r (25 U |w| + 84 |x r| M).
-  gain_rows: 24 of each term U |x r|, and at most 64 additions one after the other before the chunks are added in 64 bits (16 tokens
-     of a chunk by four waves, at most 16 steps over the heads): 88 of the sum of magnitudes.
+  gain_rows: 24 of each term U |x r|, and at most 64 additions one after the other before the chunks are added in 64 bits (a wave's
+     steps over its tokens and heads: 18 in the longest of these cases): 88 of the sum of magnitudes.
   The angle itself is a product of the position with a frequency in turns, taken twice here: three roundings of 2^-53 of it come on
      top of the 24, 25, 84 and 88, which counts for positions beyond some ten millions."""
 import pytest
@@ -131,6 +131,18 @@ def test_sizes(dtype, case, pairs):
     B, T, Hs, D, rot = case
     heads, dys = make(B, T, Hs, D, dtype, seed=D)
     check(heads, dys, full(heads), full(heads), dp.rotary_freqs(rot) if rot else None, pairs=pairs)
+
+
+LONG = [(3, 9000, (8, 2), 64, 64), (7, 3001, (5, 1), 80, 40), (200, 70, (2, 2), 256, 256), (2, 20000, (9, 2), 128, 128), (9, 2600, (6, 2), 110, 110)]
+
+
+@pytest.mark.parametrize("padded", [False, True], ids=["full", "padded"])
+@pytest.mark.parametrize("case", LONG, ids=lambda c: "x".join(str(v) for v in c).replace(" ", ""))
+def test_several_tokens_of_each_wave(case, padded):
+    B, T, Hs, D, rot = case
+    lengths = torch.tensor([T - i * T // B for i in range(B - 1)] + [0], dtype=torch.int32, device="cuda") if padded else None
+    heads, dys = make(B, T, Hs, D, BF16, seed=D + 1, lengths=lengths)
+    check(heads, dys, full(heads), full(heads), dp.rotary_freqs(rot), lengths=lengths)
 
 
 @pytest.mark.parametrize("D,rot", [(64, 64), (64, 32), (24, 10)])
@@ -288,3 +300,12 @@ def test_graph_replays_and_streams():
     assert torch.equal(sq2, sq) and all(torch.equal(a, b) for a, b in zip(rows, rows2))
     with pytest.raises(ValueError):
         dp.headnorm_sqnorm(None, None, sq, freqs=freqs, descs=fwd)
+
+
+def test_shapes_of_positions():
+    heads, _ = make(3, 5, (2,), 8, F32)
+    for shape in ((3, 5), (5,)):
+        dp.headnorm(heads, freqs=dp.rotary_freqs(8), positions=torch.zeros(shape, dtype=torch.int32, device="cuda"))
+    for shape in ((5, 3), (15,), (3,), (1, 5), (3, 5, 1)):
+        with pytest.raises(ValueError):
+            dp.headnorm(heads, freqs=dp.rotary_freqs(8), positions=torch.zeros(shape, dtype=torch.int32, device="cuda"))

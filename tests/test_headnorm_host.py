@@ -26,7 +26,7 @@ def heads(*each):
     for i, over in enumerate(each):
         s = (T * 4 * D, 4 * D, D)
         d = dict(x=A + 0x100000 * i, x_b=s[0], x_t=s[1], x_h=s[2], H=4, gain=A, out=FAR + 0x100000 * i, o_b=s[0], o_t=s[1], o_h=s[2],
-                 dy=FAR2 + 0x100000 * i, dy_b=s[0], dy_t=s[1], dy_h=s[2], gain_rows=A)
+                 dy=FAR2 + 0x100000 * i, dy_b=s[0], dy_t=s[1], dy_h=s[2], gain_rows=A + 0x1000 * i)
         arr[i] = dp.HeadsDesc(**{**d, **over})
     return arr
 
@@ -71,6 +71,21 @@ def test_addresses_and_strides(lib):
         assert back(lib, h=heads({name: 1 << 50})) == NO, name
     assert back(lib, h=heads({"x_b": 0, "x_t": 0, "x_h": 0})) == OK                 # a broadcast input
     assert back(lib, h=heads({"o_t": 0})) == BAD and back(lib, h=heads({"o_h": 7})) == BAD
+
+
+def test_each_descriptor_has_rows_of_its_own(lib):
+    size = 4 * B * D
+    assert back(lib, h=heads({}, {"gain_rows": A})) == BAD and back(lib, h=heads({}, {"gain_rows": A + size - 4})) == BAD
+    assert back(lib, h=heads({}, {"gain_rows": A + size})) == OK
+
+
+def test_number_of_heads(lib):
+    def wide(H):
+        t, b = H * D, T * H * D
+        return dict(H=H, x_t=t, x_b=b, o_t=t, o_b=b, dy_t=t, dy_b=b, out=A, dy=1 << 40)
+    big = 1 << 20
+    assert back(lib, h=heads(wide(big))) == OK and back(lib, h=heads(wide(big + 1))) == NO
+    assert back(lib, h=heads({"H": 0}, wide(big + 1))) == NO
 
 
 def test_outputs_share_nothing(lib):

@@ -67,6 +67,16 @@ def test_add_refusals(lib):
     assert add(out=far, o_q=7, o_h=34, o_b=105) == bad
 
 
+def test_size_of_the_table(lib):
+    # offsets of its elements are 32-bit numbers
+    H = 1 << 20
+    wide = dict(B=1, H=H, Tq=1, Tk=1, s_b=H, s_h=1, s_q=1, o_b=H, o_h=1, o_q=1)
+    assert grad(lib, n_buckets=1024, **wide) == dp.DP_ERR_WORKSPACE
+    wide["H"] += 1
+    assert grad(lib, n_buckets=1024, **wide) == dp.DP_ERR_UNSUPPORTED
+    assert lib.dp_posbias_add(desc(n_buckets=1024, **wide), A, A, dp.DP_F32, A, None) == dp.DP_ERR_UNSUPPORTED
+
+
 def test_workspace_sizes(lib):
     f = lib.dp_posbias_workspace_bytes
     assert f(0, 3, 5, 7) == f(2, 3, 0, 7) == f(-1, 3, 5, 7) == f(1 << 31, 1, 1, 1) == 0
