@@ -90,6 +90,9 @@ struct ClippedBiasDesc { const float* u; const float* clip; int D; float* grad_b
 hipError_t launch_clipped_bias_layers(const ClippedBiasDesc* layers, int n_layers, int B, bool accumulate, float stddev, uint64_t seed, hipStream_t st);
 hipError_t launch_philox_raw(uint32_t* out, int64_t n_counters, uint64_t seed, uint64_t first, hipStream_t st);
 
+// Bytes of the last-level cache
+constexpr int64_t kLastLevelCache = int64_t(256) << 20;
+
 // ---- strided tensors (dp_api_strided.hip): three dimensions (sizes of at least 1, strides >= 0) outside of `inner` elements next
 // to each other, all in elements of `es` bytes
 struct Strided { const void* p; int64_t size[3], stride[3], inner; int es; };

@@ -32,7 +32,7 @@ __device__ __forceinline__ int bucket_of(const PosbiasArgs& a, int64_t distance)
 struct AddTiles { int ct, rg, steps, row_tiles, col_tiles; };      // ct, rg: logarithms
 constexpr int kAddSteps = 8;
 constexpr int kAddDistances = 8 * (kThreads + kAddSteps);          // 8 (CT + RG steps) with CT RG = 256 threads
-template <int DT>
+template <int DT, bool PAST>
 __global__ __launch_bounds__(kThreads) void k_posbias_add(PosbiasArgs a, const void* scores, const float* __restrict__ table, void* out, AddTiles tl) {
     __shared__ __align__(16) float bias[kAddDistances];
     const int CT = 1 << tl.ct, RG = 1 << tl.rg;
@@ -123,7 +123,7 @@ __global__ __launch_bounds__(kThreads) void k_posbias_add(PosbiasArgs a, const v
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] += c[3 + j - i];
             const int n = min(nk, seen + i);
-            if (n >= 8) store8<DT>(out, to + i * a.o_q, v);
+            if (n >= 8) store8<DT, PAST>(out, to + i * a.o_q, v);
             else        store_first<DT>(out, to + i * a.o_q, max(n, 0), f32x8{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]});
         }
     }
@@ -468,9 +468,15 @@ size_t posbias_ws_bytes(int B, int H, int Tq, int Tk) {
 hipError_t launch_posbias_add(const PosbiasArgs& a, const void* scores, const float* table, int dt, void* out, hipStream_t st) {
     const AddTiles t = plan_add((int64_t)a.B * a.H, a.Tq, a.Tk);
     const unsigned grid = (unsigned)((int64_t)a.B * a.H * t.row_tiles * t.col_tiles);
-    if (dt == 0)      k_posbias_add<0><<<grid, kThreads, 0, st>>>(a, scores, table, out, t);
-    else if (dt == 1) k_posbias_add<1><<<grid, kThreads, 0, st>>>(a, scores, table, out, t);
-    else              k_posbias_add<2><<<grid, kThreads, 0, st>>>(a, scores, table, out, t);
+    // Where the scores fit the last-level cache, but not with the output, which would push them out, it goes past that cache: 160 MB
+    // and 160 MB of bf16, 5 x 4096 x 4096, 51 us instead of 65.  (Larger scores do not stay there either way: 394 MB 168 us instead of
+    // 170.  float32 has stores of 16 bytes 32 bytes apart, which the cache puts together: 80 x 2 x 512 x 512 73 us instead of 64.)
+    const int64_t bytes = (int64_t)a.B * a.H * a.Tq * a.Tk * 2;
+    const bool past = out != scores && bytes <= kLastLevelCache && 2 * bytes > kLastLevelCache;
+    const auto run = [&](auto kernel) { kernel<<<grid, kThreads, 0, st>>>(a, scores, table, out, t); };
+    if (dt == 0)      run(k_posbias_add<0, false>);
+    else if (dt == 1) run(past ? k_posbias_add<1, true> : k_posbias_add<1, false>);
+    else              run(past ? k_posbias_add<2, true> : k_posbias_add<2, false>);
     return hipGetLastError();
 }
 

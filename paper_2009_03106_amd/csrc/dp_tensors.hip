@@ -235,13 +235,13 @@ hipError_t place_items(const TensorItem* items, int n, void* ws, hipStream_t st,
     return hipGetLastError();
 }
 
-// Whether the outputs are larger than the 256 MB of the last-level cache: nothing that reads them behind the call finds them there.
+// Whether the outputs are larger than the last-level cache: nothing that reads them behind the call finds them there.
 // (340 MB of float32: 221 us with plain stores in the order of the norm, 192 us past the cache and from the end; smaller
 // outputs stay, for the optimizer step that reads them next.)
 bool past_cache(const TensorItem* items, int n) {
     int64_t bytes = 0;
     for (int i = 0; i < n; ++i) bytes += items[i].n * (items[i].odt == 0 ? 4 : 2);
-    return bytes > int64_t(256) << 20;
+    return bytes > kLastLevelCache;
 }
 
 // Up to here every workgroup of the scaling launch adds up the chunks' sums by itself
