@@ -7,6 +7,7 @@
 // A row of D numbers is the registers of L lanes of a wave, as pairs that turn together; the 64 / L rows of a wave are `hw`
 // heads of `tw` tokens, hw tw = 64 / L.  The sines and cosines of a token's angles serve all of its heads.
 #include <algorithm>
+#include <type_traits>
 #include "dp_elems.h"
 #include "dp_internal.h"
 
@@ -22,8 +23,10 @@ struct Rows {
 };
 
 // A lane has two pieces of eight numbers (16 bytes; float32: 32), eight pairs.
-//   halves: columns 8 l and rot / 2 + 8 l, as far as the numbers turn; behind them 16 numbers next to each other
-//   PAIRS:  columns 16 l to 16 l + 15, neighbours turn together
+//   halves: columns 8 l and rot / 2 + 8 l, as far as the numbers turn
+//   PAIRS (neighbours turn together), and behind the numbers that turn: the first pieces of all lanes, then the second ones, so that
+//           the lanes' pieces lie next to each other in every access (48 us for 122 MB of 24 + 8 heads of 64 float32; with the 16 numbers
+//           of a lane next to each other 58)
 // na, nb: how many of each piece there are (WHOLE: eight, or none for lanes behind the row).
 struct Pieces { int a, b, na, nb; };
 template <bool PAIRS, bool WHOLE> __device__ __forceinline__ Pieces pieces(const HeadnormArgs& a, int l) {
@@ -34,10 +37,11 @@ template <bool PAIRS, bool WHOLE> __device__ __forceinline__ Pieces pieces(const
         p.b = half + 8 * l;
         p.na = p.nb = WHOLE ? 8 : min(8, half - 8 * l);
     } else {
-        p.a = (PAIRS ? 0 : a.rot) + 16 * (l - turning);
-        p.b = p.a + 8;
-        p.na = WHOLE ? (p.a < a.D ? 8 : 0) : min(8, max(0, a.D - p.a));
-        p.nb = WHOLE ? p.na : min(8, max(0, a.D - p.b));
+        const int first = PAIRS ? 0 : a.rot, lanes = (a.D - first + 15) / 16, k = l - turning;
+        p.a = first + 8 * k;
+        p.b = first + 8 * (lanes + k);
+        p.na = k >= lanes ? 0 : WHOLE ? 8 : min(8, a.D - p.a);
+        p.nb = k >= lanes ? 0 : WHOLE ? 8 : min(8, max(0, a.D - p.b));
     }
     return p;
 }
@@ -67,8 +71,8 @@ template <int DT, bool WHOLE> __device__ __forceinline__ void load_some(const vo
         load_first<DT>(p, row + c, n, v);
     }
 }
-template <int DT, bool WHOLE> __device__ __forceinline__ void store_some(void* p, int64_t at, int n, const float (&v)[8]) {
-    if (n == 8)      store8<DT>(p, at, v);
+template <int DT, bool WHOLE, bool PAST> __device__ __forceinline__ void store_some(void* p, int64_t at, int n, const float (&v)[8]) {
+    if (n == 8)      store8<DT, PAST>(p, at, v);
     else if (!WHOLE) store_first<DT>(p, at, n, f32x8{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]});
 }
 
@@ -80,9 +84,9 @@ template <int DT, bool PAIRS, bool WHOLE> struct Row {
         load_some<DT, WHOLE>(p, at, c.a, live ? c.na : 0, lo);
         load_some<DT, WHOLE>(p, at, c.b, live ? c.nb : 0, hi);
     }
-    __device__ __forceinline__ void store(const Pieces& c, void* p, int64_t at) const {
-        store_some<DT, WHOLE>(p, at + c.a, c.na, lo);
-        store_some<DT, WHOLE>(p, at + c.b, c.nb, hi);
+    template <bool PAST> __device__ __forceinline__ void store(const Pieces& c, void* p, int64_t at) const {
+        store_some<DT, WHOLE, PAST>(p, at + c.a, c.na, lo);
+        store_some<DT, WHOLE, PAST>(p, at + c.b, c.nb, hi);
     }
     __device__ __forceinline__ void to_lds(const Pieces& c, float* row) const {
 #pragma unroll
@@ -126,14 +130,14 @@ template <int DT, bool PAIRS, bool WHOLE> struct Row {
     }
 };
 
-// sine and cosine of position * freq.  The angle is taken in turns and in 64 bits, without its whole turns and then without its
-// nearest quarter: what is left is at most an eighth of a turn, and the series below are exact to float32 there (the first terms
-// left out: x^11 / 11! < 2e-9, x^12 / 12! < 2e-10 for x up to pi / 4).
+// sine and cosine of position * freq.  The angle is taken in quarter turns and in 64 bits, without the nearest whole number of them:
+// what is left is at most an eighth of a turn, and the series below are exact to float32 there (the first terms left out:
+// x^11 / 11! < 2e-9, x^12 / 12! < 2e-10 for x up to pi / 4).  Added to 1.5 2^52, a number below 2^51 is rounded to a whole one, whose
+// last bits are the sum's.
 __device__ __forceinline__ void sincos_of(int position, double freq, float& s, float& c) {
-    const double turns = (double)position * (freq * 0.15915494309189533577), part = turns - floor(turns);      // 0 to 1
-    const double quarter = rint(part * 4.0);
-    const float x = (float)(part - quarter * 0.25) * 6.2831853f;
-    const int q = (int)quarter & 3;
+    const double quarters = (double)position * (freq * 0.63661977236758134308), big = 6755399441055744.0, sum = quarters + big;
+    const float x = (float)(quarters - (sum - big)) * 1.5707963f;
+    const int q = (int)__double_as_longlong(sum) & 3;
     const float z = x * x;
     const float sx = x + x * z * (-1.6666667e-1f + z * (8.3333333e-3f + z * (-1.9841270e-4f + z * 2.7557319e-6f)));
     const float cx = 1.0f + z * (-0.5f + z * (4.1666667e-2f + z * (-1.3888889e-3f + z * (2.4801587e-5f + z * -2.7557319e-7f))));
@@ -143,15 +147,16 @@ __device__ __forceinline__ void sincos_of(int position, double freq, float& s, f
     if (q == 1 || q == 2) c = -c;
 }
 
-// the turn of each pair of a lane, pairs 8 l to 8 l + 7; those behind the rotated ones do not turn
-struct Turn {
+// the turn of each pair of a lane; those behind the rotated ones do not turn
+template <bool PAIRS> struct Turn {
     float s[8], c[8];
-    __device__ __forceinline__ void of(const HeadnormArgs& a, int position, int l, bool live) {
+    __device__ __forceinline__ void of(const HeadnormArgs& a, const Pieces& p, int position, bool live) {
 #pragma unroll
         for (int v = 0; v < 8; ++v) {
             s[v] = 0.f;
             c[v] = 1.f;
-            if (live && 8 * l + v < a.rot / 2) sincos_of(position, a.freqs[8 * l + v], s[v], c[v]);
+            const int j = !PAIRS ? p.a + v : v < 4 ? p.a / 2 + v : p.b / 2 + v - 4;
+            if (live && j < a.rot / 2) sincos_of(position, a.freqs[j], s[v], c[v]);
         }
     }
 };
@@ -174,7 +179,7 @@ __device__ __forceinline__ Token token_of(const HeadnormArgs& a, int n) {      /
 }
 
 // A wave takes tw tokens at a time and its share of the steps over their heads.
-template <int DT, bool PAIRS, bool WHOLE>
+template <int DT, bool PAIRS, bool WHOLE, bool PAST>
 __global__ __launch_bounds__(kThreads) void k_headnorm(HeadnormArgs a, Rows w) {
     const int lane = threadIdx.x & (kWave - 1), l = lane & (w.L - 1), g = lane / w.L;
     const int64_t wave = (int64_t)blockIdx.x * (kThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -185,8 +190,8 @@ __global__ __launch_bounds__(kThreads) void k_headnorm(HeadnormArgs a, Rows w) {
     const float mean = 1.0f / a.D;
     for (int64_t n0 = wave / w.split * w.tw; n0 < a.B * a.T; n0 += step * w.tw) {
         const Token k = token_of(a, (int)n0 + g / w.hw);
-        Turn turn;
-        turn.of(a, k.position, l, k.live);
+        Turn<PAIRS> turn;
+        turn.of(a, pc, k.position, k.live);
 #pragma unroll 1
         for (int which = it0 >= w.its0; which <= (it1 > w.its0); ++which) {
             const HeadsArgs& hd = a.heads[which];
@@ -209,7 +214,7 @@ __global__ __launch_bounds__(kThreads) void k_headnorm(HeadnormArgs a, Rows w) {
                     x.hi[i] *= r * gain.hi[i];
                 }
                 x.rotate(turn.s, turn.c, 1.0f);
-                if (live) x.store(pc, hd.out, out + h * hd.o_h);
+                if (live) x.template store<PAST>(pc, hd.out, out + h * hd.o_h);
             }
         }
     }
@@ -226,7 +231,7 @@ struct Back {
 };
 struct BackPlan { Back of[2]; int first; };            // workgroups from `first` on have the second descriptor's heads
 
-template <int DT, bool PAIRS, bool WHOLE>
+template <int DT, bool PAIRS, bool WHOLE, bool PAST>
 __global__ __launch_bounds__(kThreads, 3) void k_headnorm_back(HeadnormArgs a, BackPlan plan) {
     __shared__ float sums[kThreads / kWave][kMaxHeadDim];
     __shared__ __align__(16) float gains[kMaxHeadDim]; // not in registers, which decide how many waves there are
@@ -246,12 +251,12 @@ __global__ __launch_bounds__(kThreads, 3) void k_headnorm_back(HeadnormArgs a, B
     for (int j = threadIdx.x; j < a.D; j += kThreads) gains[j] = global_in<float>(hd.gain)[j];
     __syncthreads();
     Row<0, PAIRS, WHOLE> acc = {};
-    Turn turn;
+    Turn<PAIRS> turn;
     const int64_t x0 = b * hd.x_b, u0 = b * hd.dy_b, o0 = b * hd.o_b;
     for (int64_t n = t0 + wave / w.split * w.tw; n < end; n += step) {
         const int64_t t = n + g / w.hw;                // the lane's token
         const bool here = t < end;
-        turn.of(a, !here ? 0 : a.positions ? a.positions[b * a.positions_b + t] : (int)t, l, here);
+        turn.of(a, pc, !here ? 0 : a.positions ? a.positions[b * a.positions_b + t] : (int)t, here);
         for (int it = it0; it < it1; ++it) {
             const int h = it * w.hw + (g & (w.hw - 1));
             const bool live = here && h < hd.H;
@@ -283,7 +288,7 @@ __global__ __launch_bounds__(kThreads, 3) void k_headnorm_back(HeadnormArgs a, B
                 x.lo[i] = r * (u.lo[i] - x.lo[i] * dot);
                 x.hi[i] = r * (u.hi[i] - x.hi[i] * dot);
             }
-            if (live) x.store(pc, hd.out, o0 + t * hd.o_t + h * hd.o_h);
+            if (live) x.template store<PAST>(pc, hd.out, o0 + t * hd.o_t + h * hd.o_h);
         }
     }
     // the rows of a wave, then the waves, in a fixed order
@@ -403,9 +408,10 @@ Rows rows_of(int H0, int H1, int L, int turns) {
 
 // Chunks of an example's tokens in the backward pass.  The chip holds 768 workgroups at a time (three for each of the 256 compute
 // units by registers, four for some types), and a launch takes about as many rounds of 768 as it has, of the steps of a wave (a row
-// for each of its groups of lanes) and about four more for its beginning and its end.  29 examples of up to 7231 tokens of 5 + 1
-// heads of 64 bf16: 94 us so, 107 us in rounds of 1024, 98 us in 1536 workgroups whatever the sizes.
-constexpr int kAtATime = 768, kMostRounds = 6, kBackChunks = 512, kEndSteps = 4;
+// for each of its groups of lanes), about two more for each token's angles, and about four for its beginning and its end.
+// 11 x 1688 tokens, padded, of 32 + 8 heads of 96 fp16: 77 us, 84 in rounds of 1024.  2 x 54613 tokens of 5 + 1 heads of 128 bf16: 124
+// us, 140 with the angles not counted.  1 x 109226 of them: 134 us, 168 with a third of the chunks at most.
+constexpr int kAtATime = 768, kMostRounds = 6, kBackChunks = 1536, kEndSteps = 4, kAngleSteps = 2;
 int most_chunks(int B, int T) { return std::max(1, std::min({kBackChunks, T, kMostRounds * kAtATime / B})); }
 
 // A wave gets about per_wave steps: descriptors with more heads get shorter chunks; where tokens are few, two or four waves of a
@@ -419,7 +425,7 @@ BackCost cut_back(const HeadnormArgs& a, int64_t per_wave, BackPlan& p) {
         Back& k = p.of[i];
         k.w.split = 1;
         while (k.w.split < waves && k.w.split * 2 <= k.w.its && k.w.its / k.w.split > per_wave) k.w.split *= 2;
-        const int granule = waves / k.w.split * k.w.tw, its = ceil_div(std::max(1, k.w.its), k.w.split);      // tokens that a workgroup has at a time, steps for them
+        const int granule = waves / k.w.split * k.w.tw, its = ceil_div(std::max(1, k.w.its), k.w.split) + kAngleSteps;      // tokens that a workgroup has at a time, steps for them
         const int64_t rounds = std::max<int64_t>({1, per_wave / its, ceil_div(ceil_div(a.T, granule), most)});
         k.tokens = (int)std::min<int64_t>(a.T, granule * rounds);
         k.chunks = ceil_div(a.T, k.tokens);
@@ -434,7 +440,7 @@ BackPlan plan_back(const HeadnormArgs& a, int L, float* partial) {
     for (int i = 0; i < a.n_heads; ++i) {
         p.of[i].w = rows_of(a.heads[i].H, 0, L, kTurns);
         p.of[i].partial = partial + (int64_t)i * a.B * most_chunks(a.B, a.T) * a.D;
-        steps += (int64_t)a.B * ceil_div(a.T, p.of[i].w.tw) * p.of[i].w.its;
+        steps += (int64_t)a.B * ceil_div(a.T, p.of[i].w.tw) * (p.of[i].w.its + kAngleSteps);
     }
     int64_t best = INT64_MAX, best_per_wave = 1;
     for (int r = a.lengths ? 2 : 1; r <= kMostRounds; ++r) {            // (lengths: the ends of at least two rounds even out)
@@ -451,19 +457,39 @@ BackPlan plan_back(const HeadnormArgs& a, int L, float* partial) {
     return p;
 }
 
-template <int DT, bool PAIRS, bool WHOLE> void forward_as(const HeadnormArgs& a, const Rows& w, int grid, hipStream_t st) {
-    k_headnorm<DT, PAIRS, WHOLE><<<grid, kThreads, 0, st>>>(a, w);
+// Whether the outputs go past the last-level cache: where the inputs fit it, but not with the outputs, which would push them out.
+// 159 MB and as much of outputs, 30 x 32 heads of 128 bf16: 54 us instead of 71; 24 + 8 heads of 32 float32: 79 instead of 83;
+// backward, 99 MB of each: 62 us instead of 73.  Larger inputs do not stay there either way: 399 MB of 24 + 8 heads of 32 float32 took
+// 235 us past the cache and 191 through it, of 128 bf16 156 and 160.  Pieces that are not whole are stored in parts of cache
+// lines, which the cache puts together.
+bool past_cache(const HeadnormArgs& a, int dt) {
+    int64_t in = 0, out = 0;
+    for (int i = 0; i < a.n_heads; ++i) {
+        const HeadsArgs& h = a.heads[i];
+        const int64_t bytes = (int64_t)a.B * a.T * h.H * a.D * (dt == 0 ? 4 : 2);
+        in += h.dy ? 2 * bytes : bytes;
+        if (h.out != h.x && h.out != h.dy) out += bytes;
+    }
+    return whole_pieces(a) && in <= kLastLevelCache && in + out > kLastLevelCache;
 }
-template <int DT, bool PAIRS, bool WHOLE> void backward_as(const HeadnormArgs& a, const BackPlan& p, hipStream_t st) {
-    k_headnorm_back<DT, PAIRS, WHOLE><<<a.B * (p.of[0].chunks + p.of[1].chunks), kThreads, 0, st>>>(a, p);
+template <int DT, class F> void by_layout(const HeadnormArgs& a, F&& f) {
+    const bool past = past_cache(a, DT);
+    constexpr std::false_type no{};
+    constexpr std::true_type yes{};
+    const auto pairs = [&](auto p) {
+        if (!whole_pieces(a)) f(p, no, no);
+        else if (past)        f(p, yes, yes);
+        else                  f(p, yes, no);
+    };
+    if (a.pairs) pairs(yes);
+    else         pairs(no);
 }
 template <int DT> void forward(const HeadnormArgs& a, const Rows& w, int grid, hipStream_t st) {
-    if (whole_pieces(a)) a.pairs ? forward_as<DT, true, true>(a, w, grid, st) : forward_as<DT, false, true>(a, w, grid, st);
-    else                 a.pairs ? forward_as<DT, true, false>(a, w, grid, st) : forward_as<DT, false, false>(a, w, grid, st);
+    by_layout<DT>(a, [&](auto pairs, auto whole, auto past) { k_headnorm<DT, pairs, whole, past><<<grid, kThreads, 0, st>>>(a, w); });
 }
 template <int DT> void backward(const HeadnormArgs& a, const BackPlan& p, hipStream_t st) {
-    if (whole_pieces(a)) a.pairs ? backward_as<DT, true, true>(a, p, st) : backward_as<DT, false, true>(a, p, st);
-    else                 a.pairs ? backward_as<DT, true, false>(a, p, st) : backward_as<DT, false, false>(a, p, st);
+    const int grid = a.B * (p.of[0].chunks + p.of[1].chunks);
+    by_layout<DT>(a, [&](auto pairs, auto whole, auto past) { k_headnorm_back<DT, pairs, whole, past><<<grid, kThreads, 0, st>>>(a, p); });
 }
 
 }  // namespace
