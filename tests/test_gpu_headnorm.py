@@ -133,7 +133,8 @@ def test_sizes(dtype, case, pairs):
     check(heads, dys, full(heads), full(heads), dp.rotary_freqs(rot) if rot else None, pairs=pairs)
 
 
-LONG = [(3, 9000, (8, 2), 64, 64), (7, 3001, (5, 1), 80, 40), (200, 70, (2, 2), 256, 256), (2, 20000, (9, 2), 128, 128), (9, 2600, (6, 2), 110, 110)]
+LONG = [(3, 9000, (8, 2), 64, 64), (7, 3001, (5, 1), 80, 40), (200, 70, (2, 2), 256, 256), (2, 20000, (9, 2), 128, 128), (9, 2600, (6, 2), 110, 110),
+        (1, 25000, (16, 8), 128, 64)]       # 153 MB and as much of outputs: more than the last-level cache together
 
 
 @pytest.mark.parametrize("padded", [False, True], ids=["full", "padded"])

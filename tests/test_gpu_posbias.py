@@ -90,6 +90,20 @@ def test_shapes(dtype, shape, causal):
     check(x, table, buckets, causal=causal)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F16], ids=["bf16", "f16"])
+@pytest.mark.parametrize("causal", [False, True], ids=["both", "causal"])
+def test_scores_that_fit_the_cache_without_the_output(dtype, causal):
+    """162 MB and as much again, of 256 MB: the outputs take another way than those in place, which is checked elsewhere."""
+    x, table, buckets = make(3, 16, 1300, 1301, dtype, seed=12, both=not causal)
+    k_lens = torch.tensor([1301, 1000, 37], dtype=torch.int32, device="cuda")
+    out = torch.full_like(x, 77.0)
+    dp.posbias_add(x, table, buckets, out, causal=causal, k_lens=k_lens)
+    y = x.clone()
+    dp.posbias_add(y, table, buckets, causal=causal, k_lens=k_lens)
+    live = windows(3, 1300, 1301, None, None, k_lens, causal)[1].unsqueeze(1)
+    assert torch.equal(out, torch.where(live, y, 77.0)) and torch.equal(torch.where(live, 0.0, y), torch.where(live, 0.0, x))
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("Tq,Tk", [(1, 300), (77, 300), (300, 300), (520, 90)])
 @pytest.mark.parametrize("causal", [False, True], ids=["both", "causal"])
