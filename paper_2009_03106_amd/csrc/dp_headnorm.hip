@@ -27,32 +27,41 @@ struct Rows {
 //   PAIRS (neighbours turn together), and behind the numbers that turn: the first pieces of all lanes, then the second ones, so that
 //           the lanes' pieces lie next to each other in every access (48 us for 122 MB of 24 + 8 heads of 64 float32; with the 16 numbers
 //           of a lane next to each other 58)
-// na, nb: how many of each piece there are (WHOLE: eight, or none for lanes behind the row).
+// na, nb: how many of each piece there are: eight, or none for lanes behind the row (kWhole), also four (kFours), any number (kAny).
+enum Fill { kAny, kFours, kWhole };
 struct Pieces { int a, b, na, nb; };
-template <bool PAIRS, bool WHOLE> __device__ __forceinline__ Pieces pieces(const HeadnormArgs& a, int l) {
+template <bool PAIRS, Fill F> __device__ __forceinline__ Pieces pieces(const HeadnormArgs& a, int l) {
     const int half = a.rot / 2, turning = PAIRS ? 0 : (half + 7) / 8;      // lanes with pairs that are half of `rot` apart
     Pieces p;
     if (!PAIRS && l < turning) {
         p.a = 8 * l;
         p.b = half + 8 * l;
-        p.na = p.nb = WHOLE ? 8 : min(8, half - 8 * l);
+        p.na = p.nb = F == kWhole ? 8 : min(8, half - 8 * l);
     } else {
         const int first = PAIRS ? 0 : a.rot, lanes = (a.D - first + 15) / 16, k = l - turning;
         p.a = first + 8 * k;
         p.b = first + 8 * (lanes + k);
-        p.na = k >= lanes ? 0 : WHOLE ? 8 : min(8, a.D - p.a);
-        p.nb = k >= lanes ? 0 : WHOLE ? 8 : min(8, max(0, a.D - p.b));
+        p.na = k >= lanes ? 0 : F == kWhole ? 8 : min(8, a.D - p.a);
+        p.nb = k >= lanes ? 0 : F == kWhole ? 8 : min(8, max(0, a.D - p.b));
     }
     return p;
 }
 
 // n numbers of the row at `row`, from column c on.  A piece that is not whole is the end of eight numbers (where the row has as many
 // before its end), moved to the front: one load, and selects.
-template <int DT, bool WHOLE> __device__ __forceinline__ void load_some(const void* p, int64_t row, int c, int n, float (&v)[8]) {
-    if constexpr (WHOLE) {
+template <int DT, Fill F> __device__ __forceinline__ void load_some(const void* p, int64_t row, int c, int n, float (&v)[8]) {
+    if constexpr (F == kWhole) {
         Raw8<DT> r{};
         if (n) r = load_raw8<DT>(p, row + c);
         widen8<DT>(r, v);
+    } else if constexpr (F == kFours) {
+        float f[4] = {}, g[4] = {};
+        if (n) {                                       // the second four: these again, where there are no more
+            load_piece<DT>(p, row + c, f);
+            load_piece<DT>(p, row + c + (n & 8) / 2, g);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { v[j] = f[j]; v[4 + j] = n == 8 ? g[j] : 0.f; }
     } else if (n == 0 || c + n >= 8) {
         const int over = 8 - n;
         Raw8<DT> r{};
@@ -71,22 +80,28 @@ template <int DT, bool WHOLE> __device__ __forceinline__ void load_some(const vo
         load_first<DT>(p, row + c, n, v);
     }
 }
-template <int DT, bool WHOLE, bool PAST> __device__ __forceinline__ void store_some(void* p, int64_t at, int n, const float (&v)[8]) {
-    if (n == 8)      store8<DT, PAST>(p, at, v);
-    else if (!WHOLE) store_first<DT>(p, at, n, f32x8{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]});
+template <int DT, Fill F, bool PAST> __device__ __forceinline__ void store_some(void* p, int64_t at, int n, const float (&v)[8]) {
+    if (n == 8) {
+        store8<DT, PAST>(p, at, v);
+    } else if constexpr (F == kFours) {
+        const float f[4] = {v[0], v[1], v[2], v[3]};
+        if (n == 4) store_piece<DT>(p, at, f);
+    } else if constexpr (F == kAny) {
+        store_first<DT>(p, at, n, f32x8{v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]});
+    }
 }
 
-template <int DT, bool PAIRS, bool WHOLE> struct Row {
+template <int DT, bool PAIRS, Fill F> struct Row {
     float lo[8], hi[8];        // (lo[i], hi[i]) turn together; PAIRS: neighbours within lo, and within hi
 
     // zeros where there are none
     __device__ __forceinline__ void load(const Pieces& c, const void* p, int64_t at, bool live) {
-        load_some<DT, WHOLE>(p, at, c.a, live ? c.na : 0, lo);
-        load_some<DT, WHOLE>(p, at, c.b, live ? c.nb : 0, hi);
+        load_some<DT, F>(p, at, c.a, live ? c.na : 0, lo);
+        load_some<DT, F>(p, at, c.b, live ? c.nb : 0, hi);
     }
     template <bool PAST> __device__ __forceinline__ void store(const Pieces& c, void* p, int64_t at) const {
-        store_some<DT, WHOLE, PAST>(p, at + c.a, c.na, lo);
-        store_some<DT, WHOLE, PAST>(p, at + c.b, c.nb, hi);
+        store_some<DT, F, PAST>(p, at + c.a, c.na, lo);
+        store_some<DT, F, PAST>(p, at + c.b, c.nb, hi);
     }
     __device__ __forceinline__ void to_lds(const Pieces& c, float* row) const {
 #pragma unroll
@@ -96,10 +111,10 @@ template <int DT, bool PAIRS, bool WHOLE> struct Row {
         }
     }
     __device__ __forceinline__ void from_lds(const Pieces& c, const float* row) {
-        if constexpr (WHOLE) {                         // pieces begin on 32 bytes; lanes behind the row read a piece and drop it
+        if constexpr (F != kAny) {                     // on 16 bytes; where there is none, something of the row, which meets zeros only
             const float4* p = reinterpret_cast<const float4*>(row + (c.na ? c.a : 0));
-            const float4* q = reinterpret_cast<const float4*>(row + (c.na ? c.b : 0));
-            const float4 f[4] = {p[0], p[1], q[0], q[1]};
+            const float4* q = reinterpret_cast<const float4*>(row + (c.nb ? c.b : 0));
+            const float4 f[4] = {p[0], p[F == kWhole || c.na > 4], q[0], q[F == kWhole || c.nb > 4]};
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 lo[4 * i] = f[i].x; lo[4 * i + 1] = f[i].y; lo[4 * i + 2] = f[i].z; lo[4 * i + 3] = f[i].w;
@@ -179,14 +194,14 @@ __device__ __forceinline__ Token token_of(const HeadnormArgs& a, int n) {      /
 }
 
 // A wave takes tw tokens at a time and its share of the steps over their heads.
-template <int DT, bool PAIRS, bool WHOLE, bool PAST>
+template <int DT, bool PAIRS, Fill F, bool PAST>
 __global__ __launch_bounds__(kThreads) void k_headnorm(HeadnormArgs a, Rows w) {
     const int lane = threadIdx.x & (kWave - 1), l = lane & (w.L - 1), g = lane / w.L;
     const int64_t wave = (int64_t)blockIdx.x * (kThreads / kWave) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t step = (int64_t)gridDim.x * (kThreads / kWave) / w.split;
     const int part = (int)(wave % w.split);
     const int it0 = (int)((int64_t)w.its * part / w.split), it1 = (int)((int64_t)w.its * (part + 1) / w.split);
-    const Pieces pc = pieces<PAIRS, WHOLE>(a, l);
+    const Pieces pc = pieces<PAIRS, F>(a, l);
     const float mean = 1.0f / a.D;
     for (int64_t n0 = wave / w.split * w.tw; n0 < a.B * a.T; n0 += step * w.tw) {
         const Token k = token_of(a, (int)n0 + g / w.hw);
@@ -196,13 +211,13 @@ __global__ __launch_bounds__(kThreads) void k_headnorm(HeadnormArgs a, Rows w) {
         for (int which = it0 >= w.its0; which <= (it1 > w.its0); ++which) {
             const HeadsArgs& hd = a.heads[which];
             const int first = which ? w.its0 : 0, from = max(it0, first), to = which ? it1 : min(it1, w.its0);
-            Row<0, PAIRS, WHOLE> gain;
+            Row<0, PAIRS, F> gain;
             gain.load(pc, hd.gain, 0, true);
             const int64_t in = k.b * hd.x_b + k.t * hd.x_t, out = k.b * hd.o_b + k.t * hd.o_t;
             for (int it = from; it < to; ++it) {
                 const int h = (it - first) * w.hw + (g & (w.hw - 1));
                 const bool live = k.live && h < hd.H;
-                Row<DT, PAIRS, WHOLE> x;
+                Row<DT, PAIRS, F> x;
                 x.load(pc, hd.x, in + h * hd.x_h, live);
                 float sq = 0.f;
 #pragma unroll
@@ -231,7 +246,7 @@ struct Back {
 };
 struct BackPlan { Back of[2]; int first; };            // workgroups from `first` on have the second descriptor's heads
 
-template <int DT, bool PAIRS, bool WHOLE, bool PAST>
+template <int DT, bool PAIRS, Fill F, bool PAST>
 __global__ __launch_bounds__(kThreads, 3) void k_headnorm_back(HeadnormArgs a, BackPlan plan) {
     __shared__ float sums[kThreads / kWave][kMaxHeadDim];
     __shared__ __align__(16) float gains[kMaxHeadDim]; // not in registers, which decide how many waves there are
@@ -246,11 +261,11 @@ __global__ __launch_bounds__(kThreads, 3) void k_headnorm_back(HeadnormArgs a, B
     const int64_t t0 = (int64_t)chunk * bk.tokens;
     const int end = (int)min(t0 + bk.tokens, (int64_t)(a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T));
     const int step = kThreads / kWave / w.split * w.tw;
-    const Pieces pc = pieces<PAIRS, WHOLE>(a, l);
+    const Pieces pc = pieces<PAIRS, F>(a, l);
     const float mean = 1.0f / a.D;
     for (int j = threadIdx.x; j < a.D; j += kThreads) gains[j] = global_in<float>(hd.gain)[j];
     __syncthreads();
-    Row<0, PAIRS, WHOLE> acc = {};
+    Row<0, PAIRS, F> acc = {};
     Turn<PAIRS> turn;
     const int64_t x0 = b * hd.x_b, u0 = b * hd.dy_b, o0 = b * hd.o_b;
     for (int64_t n = t0 + wave / w.split * w.tw; n < end; n += step) {
@@ -260,7 +275,7 @@ __global__ __launch_bounds__(kThreads, 3) void k_headnorm_back(HeadnormArgs a, B
         for (int it = it0; it < it1; ++it) {
             const int h = it * w.hw + (g & (w.hw - 1));
             const bool live = here && h < hd.H;
-            Row<DT, PAIRS, WHOLE> x, u;
+            Row<DT, PAIRS, F> x, u;
             x.load(pc, hd.x, x0 + t * hd.x_t + h * hd.x_h, live);
             u.load(pc, hd.dy, u0 + t * hd.dy_t + h * hd.dy_h, live);
             float sq = 0.f;
@@ -268,7 +283,7 @@ __global__ __launch_bounds__(kThreads, 3) void k_headnorm_back(HeadnormArgs a, B
             for (int i = 0; i < 8; ++i) sq += x.lo[i] * x.lo[i] + x.hi[i] * x.hi[i];
             const float r = rsqrtf(row_sum(sq, w.L) * mean + a.eps);
             u.rotate(turn.s, turn.c, -1.0f);
-            Row<0, PAIRS, WHOLE> gain;
+            Row<0, PAIRS, F> gain;
             asm volatile("" ::: "memory");             // else the reads move out of the loops, and into registers
             gain.from_lds(pc, gains);
             float dot = 0.f;
@@ -381,9 +396,13 @@ int pow2_up(int n) {
 int lanes_of(const HeadnormArgs& a) {
     return pow2_up(a.pairs ? ceil_div(a.D, 16) : ceil_div(a.rot / 2, 8) + ceil_div(a.D - a.rot, 16));
 }
-// Whether every lane's pieces are whole.  (Others take rows whose ends are loaded and stored in smaller pieces.  Numbers one by one
-// for those, a row per wave, took 173 us instead of 87 for the backward pass of 58 x 305 tokens of 8 + 8 heads of 110 bf16.)
-bool whole_pieces(const HeadnormArgs& a) { return a.D % 16 == 0 && (a.pairs || a.rot % 16 == 0); }
+// What the lanes' pieces are.  24 + 8 heads of 72, 80 MB, forward and backward: fours 36 and 60 us in float32, 48 and 114 in bf16; any
+// number 46 and 88, 64 and 132.  (Numbers one by one, a row per wave, instead of any number: 173 us instead of 87 for the backward
+// pass of 58 x 305 tokens of 8 + 8 heads of 110 bf16.)
+Fill fill_of(const HeadnormArgs& a) {
+    if (a.D % 16 == 0 && (a.pairs || a.rot % 16 == 0)) return kWhole;
+    return a.D % 4 == 0 && (a.pairs || a.rot % 8 == 0) ? kFours : kAny;
+}
 
 constexpr int kTurns = 4;
 // Heads and tokens of a wave.  Heads lie next to each other, but the rows of a token have the same angles: as many heads at a time as
@@ -470,26 +489,30 @@ bool past_cache(const HeadnormArgs& a, int dt) {
         in += h.dy ? 2 * bytes : bytes;
         if (h.out != h.x && h.out != h.dy) out += bytes;
     }
-    return whole_pieces(a) && in <= kLastLevelCache && in + out > kLastLevelCache;
+    return fill_of(a) == kWhole && in <= kLastLevelCache && in + out > kLastLevelCache;
 }
-template <int DT, class F> void by_layout(const HeadnormArgs& a, F&& f) {
-    const bool past = past_cache(a, DT);
+template <Fill F> using FillIs = std::integral_constant<Fill, F>;
+template <int DT, class L> void by_layout(const HeadnormArgs& a, L&& launch) {
     constexpr std::false_type no{};
     constexpr std::true_type yes{};
-    const auto pairs = [&](auto p) {
-        if (!whole_pieces(a)) f(p, no, no);
-        else if (past)        f(p, yes, yes);
-        else                  f(p, yes, no);
+    const auto with = [&](auto pairs) {
+        switch (fill_of(a)) {
+        case kAny:   launch(pairs, FillIs<kAny>{}, no); break;
+        case kFours: launch(pairs, FillIs<kFours>{}, no); break;
+        default:
+            if (past_cache(a, DT)) launch(pairs, FillIs<kWhole>{}, yes);
+            else                   launch(pairs, FillIs<kWhole>{}, no);
+        }
     };
-    if (a.pairs) pairs(yes);
-    else         pairs(no);
+    if (a.pairs) with(yes);
+    else         with(no);
 }
 template <int DT> void forward(const HeadnormArgs& a, const Rows& w, int grid, hipStream_t st) {
-    by_layout<DT>(a, [&](auto pairs, auto whole, auto past) { k_headnorm<DT, pairs, whole, past><<<grid, kThreads, 0, st>>>(a, w); });
+    by_layout<DT>(a, [&](auto pairs, auto fill, auto past) { k_headnorm<DT, pairs, fill, past><<<grid, kThreads, 0, st>>>(a, w); });
 }
 template <int DT> void backward(const HeadnormArgs& a, const BackPlan& p, hipStream_t st) {
     const int grid = a.B * (p.of[0].chunks + p.of[1].chunks);
-    by_layout<DT>(a, [&](auto pairs, auto whole, auto past) { k_headnorm_back<DT, pairs, whole, past><<<grid, kThreads, 0, st>>>(a, p); });
+    by_layout<DT>(a, [&](auto pairs, auto fill, auto past) { k_headnorm_back<DT, pairs, fill, past><<<grid, kThreads, 0, st>>>(a, p); });
 }
 
 }  // namespace

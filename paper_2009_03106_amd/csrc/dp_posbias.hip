@@ -391,8 +391,8 @@ __global__ __launch_bounds__(kFinishThreads) void k_posbias_finish(PosbiasArgs a
 //
 // The workgroups of a head: the chip holds 768 at a time (three for each of the 256 compute units, by registers), and the loads of all
 // of them together are what bounds it, so that a launch takes as many rounds of 768 as it has, of a workgroup's longest piece and
-// about two steps for its fold.  The fewest steps so counted: 64 x 12 heads of 512 x 512 as 768 workgroups took 89 us, as 3072
-// 103 us.  Examples of their own lengths: two rounds at least, whose ends even out (4 x 16 heads of up to 4096 x 4096, causal: 121 us
+// about two steps for its fold.  The fewest steps so counted: 64 x 12 heads of 512 x 512 as 768 workgroups took 89 us, as four
+// times as many 103 us.  Examples of their own lengths: two rounds at least, whose ends even out (4 x 16 heads of up to 4096 x 4096, causal: 121 us
 // in two rounds, 129 in three, 168 in five).
 constexpr int kAtATime = 768, kMostRounds = 8, kFoldSteps = 2;
 // rows of a band where everything is live

@@ -121,6 +121,7 @@ CASES = [  # B, T, heads, D, rot
     (1, 300, (4, 4), 128, 64), (2, 13, (7, 1), 130, 66), (1, 37, (16, 2), 256, 256), (1, 5, (3,), 200, 200), (1, 7, (2, 1), 511, 510),
     (1, 4, (2, 3), 512, 512), (1, 3, (1, 2), 509, 6), (2, 9, (4, 1), 110, 110), (1, 33, (2, 5), 118, 38), (300, 2, (1, 1), 32, 32), (1, 2000, (1,), 64, 32), (3000, 1, (2, 1), 16, 16),
     (2, 31, (0, 3), 48, 16), (2, 11, (3, 0), 48, 32), (1, 4, (16, 16), 112, 112), (2, 70, (5, 3), 176, 96),
+    (2, 31, (5, 2), 72, 72), (1, 9, (4, 1), 4, 0), (3, 8, (2, 2), 12, 8), (1, 6, (2,), 508, 504), (2, 21, (3, 1), 100, 48),
 ]
 
 
