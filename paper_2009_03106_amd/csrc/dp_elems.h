@@ -72,9 +72,11 @@ template <int DT, bool PAST = false> __device__ __forceinline__ void store8(void
     }
 }
 
-// The first n of eight elements, 0 < n < 8, in pieces of 4, 2 and 1: zeros behind them, and nothing behind them is touched.
+// 1, 2, 4 or 8 elements
 template <int DT, int N> __device__ __forceinline__ void load_piece(const void* p, int64_t k, float (&v)[N]) {
-    if constexpr (N == 1) {
+    if constexpr (N == 8) {
+        load8<DT>(p, k, v);
+    } else if constexpr (N == 1) {
         v[0] = load_one<DT>(p, k);
     } else if constexpr (DT == 0) {
         typedef uint32_t piece __attribute__((ext_vector_type(N), aligned(4)));
@@ -93,15 +95,18 @@ template <int DT, int N> __device__ __forceinline__ void load_piece(const void* 
         for (int j = 0; j < N / 2; ++j) { v[2 * j] = In16<DT == 2>::lo(r[j]); v[2 * j + 1] = In16<DT == 2>::hi(r[j]); }
     }
 }
-template <int DT, int N> __device__ __forceinline__ void store_piece(void* p, int64_t k, const float (&v)[N]) {
-    if constexpr (N == 1) {
+template <int DT, bool PAST = false, int N> __device__ __forceinline__ void store_piece(void* p, int64_t k, const float (&v)[N]) {
+    static_assert(!PAST || N >= 4);
+    if constexpr (N == 8) {
+        store8<DT, PAST>(p, k, v);
+    } else if constexpr (N == 1) {
         store_one<DT>(p, k, v[0]);
     } else if constexpr (DT == 0) {
         typedef uint32_t piece __attribute__((ext_vector_type(N), aligned(4)));
         piece r;
 #pragma unroll
         for (int j = 0; j < N; ++j) r[j] = __float_as_uint(v[j]);
-        *global_out<piece>(static_cast<float*>(p) + k) = r;
+        store_raw<PAST>(r, global_out<piece>(static_cast<float*>(p) + k));
     } else if constexpr (N == 2) {
         typedef uint32_t piece __attribute__((aligned(2)));
         *global_out<piece>(static_cast<uint16_t*>(p) + k) = In16<DT == 2>::pack(v[0], v[1]);
@@ -110,9 +115,10 @@ template <int DT, int N> __device__ __forceinline__ void store_piece(void* p, in
         piece r;
 #pragma unroll
         for (int j = 0; j < N / 2; ++j) r[j] = In16<DT == 2>::pack(v[2 * j], v[2 * j + 1]);
-        *global_out<piece>(static_cast<uint16_t*>(p) + k) = r;
+        store_raw<PAST>(r, global_out<piece>(static_cast<uint16_t*>(p) + k));
     }
 }
+// The first n of eight elements, 0 < n < 8, in pieces of 4, 2 and 1: zeros behind them, and nothing behind them is touched.
 template <int DT> __device__ __forceinline__ void load_first(const void* p, int64_t k, int n, float (&v)[8]) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = 0.f;

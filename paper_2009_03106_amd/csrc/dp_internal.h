@@ -108,7 +108,8 @@ bool same_layout(const Strided& a, const Strided& b);
 // ---- norm and clipping of a gradient of many tensors (dp_tensors.hip)
 struct TensorItem { const void* x; void* out; int64_t n; int first_chunk; short dt, odt; };      // types as above
 constexpr int kTensorChunk = 4096;     // elements of the smallest chunk
-constexpr int kTensorChunks = 2048;    // chunks that a large set is cut into (one more at most for each tensor)
+constexpr int kTensorChunks = 2048;    // chunks that a set is cut into (one more at most for each tensor)
+constexpr int kTensorChunksLarge = 16384;              // and one of at least as many of the smallest ones
 int64_t tensor_chunk_elems(int64_t total);
 size_t tensors_ws_bytes(int64_t n_tensors);
 // first_chunk of every item is set (the items have at least one chunk each), `chunks` their number; norm != nullptr: take it

@@ -118,25 +118,50 @@ __global__ __launch_bounds__(kThreads) void k_tensors_fold(ItemTable t, const Te
     if (i < n) item_norm(partial, items[i].first_chunk, i + 1 < n ? items[i + 1].first_chunk : chunks, tensor_norms + i);
 }
 
+// From the chunk's end, which the last-level cache got last.  Four pieces in flight, of 16 bytes where they are stored, next to each other
+// for neighbouring threads.  (340 MB of float32 in 2048 chunks: 176 us for the call, 192 with pieces of 32 bytes one at a time from the
+// beginning.  2 GB, most of it bf16: 1213 us, 1284 one at a time.)
 template <int DT, int ODT, bool PAST> __device__ __forceinline__ void scale(const void* x, void* out, int64_t begin, int64_t end, float f, bool accumulate, int tid) {
-    int64_t k = begin + tid * 8;
-    for (; k + 8 <= end; k += 8 * kThreads) {
-        float v[8];
-        load8<DT>(x, k, v);
+    constexpr int V = ODT == 0 ? 4 : 8, U = 4;
+    constexpr int64_t step = V * kThreads;
+    const auto put = [&](int64_t k, float (&v)[V]) {
         if (accumulate) {
-            float o[8];
-            load8<ODT>(out, k, o);
+            float o[V];
+            load_piece<ODT>(out, k, o);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = o[j] + f * v[j];
+            for (int j = 0; j < V; ++j) v[j] = o[j] + f * v[j];
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] *= f;
+            for (int j = 0; j < V; ++j) v[j] *= f;
         }
-        store8<ODT, PAST>(out, k, v);
+        store_piece<ODT, PAST>(out, k, v);
+    };
+    int64_t m = (end - begin + step - 1) / step - 1;   // pieces of all threads together
+    if (m >= 0 && begin + (m + 1) * step > end) {      // the last ones, not of all threads
+        int64_t k = begin + m-- * step + tid * V;
+        if (k + V <= end) {
+            float v[V];
+            load_piece<DT>(x, k, v);
+            put(k, v);
+        } else {
+            for (; k < end; ++k) {
+                const float v = f * load_one<DT>(x, k);
+                store_one<ODT>(out, k, accumulate ? load_one<ODT>(out, k) + v : v);
+            }
+        }
     }
-    for (; k < end; ++k) {
-        const float v = f * load_one<DT>(x, k);
-        store_one<ODT>(out, k, accumulate ? load_one<ODT>(out, k) + v : v);
+    int64_t k = begin + m * step + tid * V;
+    for (; m >= U - 1; m -= U, k -= U * step) {
+        float v[U][V];
+#pragma unroll
+        for (int i = 0; i < U; ++i) load_piece<DT>(x, k - i * step, v[i]);
+#pragma unroll
+        for (int i = 0; i < U; ++i) put(k - i * step, v[i]);
+    }
+    for (; m >= 0; --m, k -= step) {
+        float v[V];
+        load_piece<DT>(x, k, v);
+        put(k, v);
     }
 }
 template <bool PAST> __device__ __forceinline__ void chunk_scale(const TensorItem& it, int64_t begin, int64_t chunk, float f, bool accumulate, int tid) {
@@ -162,7 +187,7 @@ __global__ __launch_bounds__(kThreads) void k_tensors_scale(ItemTable t, const T
                                                             const double* __restrict__ partial, float* __restrict__ norm, float* __restrict__ tensor_norms, float C) {
     __shared__ double red[4];
     const TensorItem* items = DIRECT ? t.items : table;
-    const int c = chunks - 1 - blockIdx.x, i = find_item(items, n, c);        // what was read last is still in the last-level cache
+    const int c = chunks - 1 - blockIdx.x, i = find_item(items, n, c);        // the last chunks are in the last-level cache (2 GB: 1213 us, 1255 from the first one)
     float total;
     if (partial) {
         total = (float)sqrt(sum_partials(partial, chunks, red));
@@ -236,8 +261,7 @@ hipError_t place_items(const TensorItem* items, int n, void* ws, hipStream_t st,
 }
 
 // Whether the outputs are larger than the last-level cache: nothing that reads them behind the call finds them there.
-// (340 MB of float32: 221 us with plain stores in the order of the norm, 192 us past the cache and from the end; smaller
-// outputs stay, for the optimizer step that reads them next.)
+// (340 MB of float32: 176 us past the cache, 212 through it; smaller outputs stay, for the optimizer step that reads them next.)
 bool past_cache(const TensorItem* items, int n) {
     int64_t bytes = 0;
     for (int i = 0; i < n; ++i) bytes += items[i].n * (items[i].odt == 0 ? 4 : 2);
@@ -267,13 +291,16 @@ void scaled(const Tables& t, int n, int64_t chunk, int chunks, bool accumulate, 
 }  // namespace
 
 // Chunks of at least 4096 elements (two 16-byte pieces of float32 for every thread), and larger ones where that makes more than
-// 2048 of them (eight workgroups for each of the 256 compute units).
+// 2048 of them (eight workgroups for each of the 256 compute units, and sums that every workgroup still adds up by itself: 31 million
+// float32 66 us, in smaller chunks and with a launch for the sums 72).  From 67 million elements on there are eight times as many:
+// the ends of the last ones matter less, and what the first pass reads last is then a part of the set, where the second one begins
+// (2 GB: 1093 us, 1213 in 2048 chunks, all of which are worked on at once).
 int64_t tensor_chunk_elems(int64_t total) {
-    const int64_t unit = 8 * kThreads;
-    return std::max<int64_t>(kTensorChunk, (total / kTensorChunks + unit) / unit * unit);
+    const int64_t unit = 8 * kThreads, most = total < (int64_t)kTensorChunk * kTensorChunksLarge ? kTensorChunks : kTensorChunksLarge;
+    return std::max<int64_t>(kTensorChunk, (total / most + unit) / unit * unit);
 }
 size_t tensors_ws_bytes(int64_t n_tensors) {
-    return table_bytes(n_tensors) + (size_t)(kTensorChunks + n_tensors + 1) * sizeof(double);
+    return table_bytes(n_tensors) + (size_t)(kTensorChunksLarge + n_tensors + 1) * sizeof(double);
 }
 
 hipError_t launch_tensors_norm(const TensorItem* items, int n, int64_t chunk, int chunks, bool accumulate, float* norm, float* tensor_norms, void* ws, hipStream_t st) {
