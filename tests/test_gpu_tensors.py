@@ -54,7 +54,7 @@ SIZES = [
     [1], [7], [8], [2049], [4096], [4097], [100000],
     [1, 2, 3, 5, 8, 13, 1000, 4095, 4096, 4097, 12289],
     [3] * 111 + [5000], [17] * 113, [1 + i % 40 for i in range(700)] + [300000],
-    [9_000_011, 5, 1_000_000, 3_000_001],
+    [9_000_011, 5, 1_000_000, 3_000_001], [40_000_003, 5, 1, 30_000_001, 9_000_000],
 ]
 
 
