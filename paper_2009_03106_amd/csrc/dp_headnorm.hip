@@ -246,20 +246,12 @@ struct Back {
 };
 struct BackPlan { Back of[2]; int first; };            // workgroups from `first` on have the second descriptor's heads
 
+// Tokens [t0, end) of example b by a workgroup: dx, and in sums[wave] the waves' shares of the gain's gradient.
 template <int DT, bool PAIRS, Fill F, bool PAST>
-__global__ __launch_bounds__(kThreads, 3) void k_headnorm_back(HeadnormArgs a, BackPlan plan) {
-    __shared__ float sums[kThreads / kWave][kMaxHeadDim];
-    __shared__ __align__(16) float gains[kMaxHeadDim]; // not in registers, which decide how many waves there are
+__device__ __forceinline__ void back_rows(const HeadnormArgs& a, const HeadsArgs& hd, const Rows& w, int b, int64_t t0, int end, float* gains, float (*sums)[kMaxHeadDim]) {
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int which = (int)blockIdx.x >= plan.first;
-    const Back& bk = plan.of[which];
-    const Rows& w = bk.w;
-    const HeadsArgs& hd = a.heads[which];
-    const int l = lane & (w.L - 1), g = lane / w.L, wg = blockIdx.x - (which ? plan.first : 0);
-    const int b = wg / bk.chunks, chunk = wg - b * bk.chunks;
+    const int l = lane & (w.L - 1), g = lane / w.L;
     const int part = wave % w.split, it0 = w.its * part / w.split, it1 = w.its * (part + 1) / w.split;
-    const int64_t t0 = (int64_t)chunk * bk.tokens;
-    const int end = (int)min(t0 + bk.tokens, (int64_t)(a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T));
     const int step = kThreads / kWave / w.split * w.tw;
     const Pieces pc = pieces<PAIRS, F>(a, l);
     const float mean = 1.0f / a.D;
@@ -315,8 +307,43 @@ __global__ __launch_bounds__(kThreads, 3) void k_headnorm_back(HeadnormArgs a, B
         }
     if (g == 0) acc.to_lds(pc, sums[wave]);
     __syncthreads();
+}
+
+__device__ __forceinline__ int length_of(const HeadnormArgs& a, int b) { return a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T; }
+
+template <int DT, bool PAIRS, Fill F, bool PAST>
+__global__ __launch_bounds__(kThreads, 3) void k_headnorm_back(HeadnormArgs a, BackPlan plan) {
+    __shared__ float sums[kThreads / kWave][kMaxHeadDim];
+    __shared__ __align__(16) float gains[kMaxHeadDim]; // not in registers, which decide how many waves there are
+    const int which = (int)blockIdx.x >= plan.first;
+    const Back& bk = plan.of[which];
+    const int wg = blockIdx.x - (which ? plan.first : 0), b = wg / bk.chunks;
+    const int64_t t0 = (int64_t)(wg - b * bk.chunks) * bk.tokens;
+    const int end = (int)min(t0 + bk.tokens, (int64_t)length_of(a, b));
+    back_rows<DT, PAIRS, F, PAST>(a, a.heads[which], bk.w, b, t0, end, gains, sums);
     for (int j = threadIdx.x; j < a.D; j += kThreads)
         bk.partial[(int64_t)wg * a.D + j] = (sums[0][j] + sums[1][j]) + (sums[2][j] + sums[3][j]);
+}
+
+// An example of few rows: a workgroup has all of them, and nothing is left to add up.
+template <int DT, bool PAIRS, Fill F>
+__global__ __launch_bounds__(kThreads, 3) void k_headnorm_back_few(HeadnormArgs a, BackPlan plan, int accumulate, float* __restrict__ sqnorm) {
+    __shared__ float sums[kThreads / kWave][kMaxHeadDim];
+    __shared__ __align__(16) float gains[kMaxHeadDim];
+    __shared__ double red[kThreads / kWave];
+    const int b = blockIdx.x, end = length_of(a, b);
+    double sq = 0.0;
+#pragma unroll 1
+    for (int which = 0; which < a.n_heads; ++which) {
+        back_rows<DT, PAIRS, F, false>(a, a.heads[which], plan.of[which].w, b, 0, end, gains, sums);
+        for (int j = threadIdx.x; j < a.D; j += kThreads) {
+            const float f = (sums[0][j] + sums[1][j]) + (sums[2][j] + sums[3][j]);
+            a.heads[which].gain_rows[(int64_t)b * a.D + j] = f;
+            sq += (double)f * f;
+        }
+    }
+    sq = block_sum_256_f64(sq, red);
+    if (threadIdx.x == 0) sqnorm[b] = (float)(accumulate ? sqnorm[b] + sq : sq);
 }
 
 // A workgroup per example: the chunks' sums (W columns next to each other for a thread, up to 64 threads along the columns, the
@@ -491,6 +518,30 @@ bool past_cache(const HeadnormArgs& a, int dt) {
     }
     return fill_of(a) == kWhole && in <= kLastLevelCache && in + out > kLastLevelCache;
 }
+// Many examples of few rows, which fill at least half of the chip with a workgroup each: the steps of a wave as above, those of the
+// fewest.  Whether there are few enough.  bf16, 4 + 1 heads of 64: 4000 examples of one token 67 us, in two launches 98; 2000 of 48 (9
+// steps) 55 and 69; 256 of 48 17 and 16; 800 of 100 (18 steps) 55 and 51.
+constexpr int kFewSteps = 10;
+bool plan_few(const HeadnormArgs& a, int L, BackPlan& p) {
+    if (a.B < kAtATime / 2) return false;
+    constexpr int waves = kThreads / kWave;
+    int64_t all = 0;
+    for (int i = 0; i < a.n_heads; ++i) {
+        int64_t least = INT64_MAX;
+        for (int turns = 1; turns <= kTurns; turns *= 2) {
+            Rows w = rows_of(a.heads[i].H, 0, L, turns);
+            for (w.split = 1; w.split <= waves && w.split <= std::max(1, w.its); w.split *= 2) {
+                const int64_t steps = (int64_t)ceil_div(a.T, waves / w.split * w.tw) * (ceil_div(w.its, w.split) + kAngleSteps);
+                if (steps >= least) continue;
+                least = steps;
+                p.of[i].w = w;
+            }
+        }
+        all += least;
+    }
+    return all <= kFewSteps;
+}
+
 template <Fill F> using FillIs = std::integral_constant<Fill, F>;
 template <int DT, class L> void by_layout(const HeadnormArgs& a, L&& launch) {
     constexpr std::false_type no{};
@@ -509,6 +560,9 @@ template <int DT, class L> void by_layout(const HeadnormArgs& a, L&& launch) {
 }
 template <int DT> void forward(const HeadnormArgs& a, const Rows& w, int grid, hipStream_t st) {
     by_layout<DT>(a, [&](auto pairs, auto fill, auto past) { k_headnorm<DT, pairs, fill, past><<<grid, kThreads, 0, st>>>(a, w); });
+}
+template <int DT> void backward_few(const HeadnormArgs& a, const BackPlan& p, bool accumulate, float* sqnorm, hipStream_t st) {
+    by_layout<DT>(a, [&](auto pairs, auto fill, auto) { k_headnorm_back_few<DT, pairs, fill><<<a.B, kThreads, 0, st>>>(a, p, accumulate, sqnorm); });
 }
 template <int DT> void backward(const HeadnormArgs& a, const BackPlan& p, hipStream_t st) {
     const int grid = a.B * (p.of[0].chunks + p.of[1].chunks);
@@ -540,6 +594,13 @@ hipError_t launch_headnorm(const HeadnormArgs& a, int dt, hipStream_t st) {
 }
 
 hipError_t launch_headnorm_sqnorm(const HeadnormArgs& a, int dt, bool accumulate, float* sqnorm, void* ws, hipStream_t st) {
+    BackPlan few{};
+    if (plan_few(a, lanes_of(a), few)) {
+        if (dt == 0)      backward_few<0>(a, few, accumulate, sqnorm, st);
+        else if (dt == 1) backward_few<1>(a, few, accumulate, sqnorm, st);
+        else              backward_few<2>(a, few, accumulate, sqnorm, st);
+        return hipGetLastError();
+    }
     const BackPlan p = plan_back(a, lanes_of(a), static_cast<float*>(ws));
     if (dt == 0)      backward<0>(a, p, st);
     else if (dt == 1) backward<1>(a, p, st);

@@ -122,6 +122,7 @@ CASES = [  # B, T, heads, D, rot
     (1, 4, (2, 3), 512, 512), (1, 3, (1, 2), 509, 6), (2, 9, (4, 1), 110, 110), (1, 33, (2, 5), 118, 38), (300, 2, (1, 1), 32, 32), (1, 2000, (1,), 64, 32), (3000, 1, (2, 1), 16, 16),
     (2, 31, (0, 3), 48, 16), (2, 11, (3, 0), 48, 32), (1, 4, (16, 16), 112, 112), (2, 70, (5, 3), 176, 96),
     (2, 31, (5, 2), 72, 72), (1, 9, (4, 1), 4, 0), (3, 8, (2, 2), 12, 8), (1, 6, (2,), 508, 504), (2, 21, (3, 1), 100, 48),
+    (400, 3, (4, 1), 72, 72), (500, 5, (3, 2), 64, 32), (450, 2, (1, 2), 110, 110), (700, 4, (0, 2), 33, 32), (390, 9, (5,), 128, 128),
 ]
 
 
@@ -132,6 +133,14 @@ def test_sizes(dtype, case, pairs):
     B, T, Hs, D, rot = case
     heads, dys = make(B, T, Hs, D, dtype, seed=D)
     check(heads, dys, full(heads), full(heads), dp.rotary_freqs(rot) if rot else None, pairs=pairs)
+
+
+@pytest.mark.parametrize("D", [64, 72, 30])
+def test_many_padded_examples(D):
+    B, T = 600, 6
+    lengths = torch.randint(-2, T + 3, (B,), dtype=torch.int32, device="cuda", generator=torch.Generator(device="cuda").manual_seed(D))
+    heads, dys = make(B, T, (4, 1), D, BF16, seed=4, lengths=lengths)
+    check(heads, dys, full(heads), full(heads), dp.rotary_freqs(D // 4 * 2), lengths=lengths)
 
 
 LONG = [(3, 9000, (8, 2), 64, 64), (7, 3001, (5, 1), 80, 40), (200, 70, (2, 2), 256, 256), (2, 20000, (9, 2), 128, 128), (9, 2600, (6, 2), 110, 110),
