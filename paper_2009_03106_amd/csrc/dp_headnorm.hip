@@ -348,16 +348,16 @@ __global__ __launch_bounds__(kThreads, 3) void k_headnorm_back_few(HeadnormArgs 
 
 // A workgroup per example: the chunks' sums (W columns next to each other for a thread, up to 64 threads along the columns, the
 // others take other chunks), and the squared norm of the rows.
-constexpr int kFoldThreads = 1024;
-template <int W>
-__global__ __launch_bounds__(kFoldThreads) void k_headnorm_fold(HeadnormArgs a, BackPlan plan, int accumulate, float* __restrict__ sqnorm) {
-    constexpr int kWaves = kFoldThreads / kWave;
+constexpr int kFoldThreads = 1024;                     // for many chunks; 256 for up to 64 (2500 x 100 tokens of 4 + 1 heads of 64 bf16: 128 us instead of 148)
+template <int W, int THREADS>
+__global__ __launch_bounds__(THREADS) void k_headnorm_fold(HeadnormArgs a, BackPlan plan, int accumulate, float* __restrict__ sqnorm) {
+    constexpr int kWaves = THREADS / kWave;
     __shared__ double part[kWaves][kWave * W];
     __shared__ double red[kWaves];
     const int b = blockIdx.x, columns = a.D / W, lane = threadIdx.x & (kWave - 1), wave = threadIdx.x >> 6;
     int ct = 1;                                        // threads along the columns, a power of two
     while (ct < columns && ct < kWave) ct *= 2;
-    const int groups = kFoldThreads / ct, g = threadIdx.x / ct;
+    const int groups = THREADS / ct, g = threadIdx.x / ct;
     double sq = 0.0;
     for (int c0 = 0; c0 < columns; c0 += ct) {
         const int c = c0 + (lane & (ct - 1));
@@ -457,7 +457,7 @@ Rows rows_of(int H0, int H1, int L, int turns) {
 // for each of its groups of lanes), about two more for each token's angles, and about four for its beginning and its end.
 // 11 x 1688 tokens, padded, of 32 + 8 heads of 96 fp16: 77 us, 84 in rounds of 1024.  2 x 54613 tokens of 5 + 1 heads of 128 bf16: 124
 // us, 140 with the angles not counted.  1 x 109226 of them: 134 us, 168 with a third of the chunks at most.
-constexpr int kAtATime = 768, kMostRounds = 6, kBackChunks = 1536, kEndSteps = 4, kAngleSteps = 2;
+constexpr int kAtATime = 768, kMostRounds = 6, kBackChunks = 1536, kEndSteps = 4, kAngleSteps = 2, kFewChunks = 64;
 int most_chunks(int B, int T) { return std::max(1, std::min({kBackChunks, T, kMostRounds * kAtATime / B})); }
 
 // A wave gets about per_wave steps: descriptors with more heads get shorter chunks; where tokens are few, two or four waves of a
@@ -607,8 +607,9 @@ hipError_t launch_headnorm_sqnorm(const HeadnormArgs& a, int dt, bool accumulate
     else              backward<2>(a, p, st);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (a.D % 4 == 0) k_headnorm_fold<4><<<a.B, kFoldThreads, 0, st>>>(a, p, accumulate, sqnorm);
-    else              k_headnorm_fold<1><<<a.B, kFoldThreads, 0, st>>>(a, p, accumulate, sqnorm);
+    const auto fold = [&](auto kernel, int threads) { kernel<<<a.B, threads, 0, st>>>(a, p, accumulate, sqnorm); };
+    if (std::max(p.of[0].chunks, p.of[1].chunks) <= kFewChunks) fold(a.D % 4 == 0 ? k_headnorm_fold<4, 256> : k_headnorm_fold<1, 256>, 256);
+    else fold(a.D % 4 == 0 ? k_headnorm_fold<4, kFoldThreads> : k_headnorm_fold<1, kFoldThreads>, kFoldThreads);
     return hipGetLastError();
 }
 
