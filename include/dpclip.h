@@ -510,7 +510,8 @@ typedef struct {
     const void* x;             /* device, `dtype`, aligned to one element: [B, T, H, D] with the strides below (in elements,
                                   >= 0), the D numbers of a row next to each other; read only unless out is x */
     int64_t x_b, x_t, x_h;
-    int64_t H;                 /* heads, at most 2^20 (queries and keys may have different numbers) */
+    int64_t H;                 /* heads, at most 2^20 (queries and keys may have different numbers); 0: x, gain, out and dy
+                                  are not looked at, and gain_rows gets zeros */
     const float* gain;         /* device float32[D] */
     void* out;                 /* device, `dtype`: y, or dx.  May be x (or dy) itself with the same strides; no other element of
                                   any out of the call is an element of an input or of another out */

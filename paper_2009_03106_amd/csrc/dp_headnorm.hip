@@ -255,7 +255,8 @@ __device__ __forceinline__ void back_rows(const HeadnormArgs& a, const HeadsArgs
     const int step = kThreads / kWave / w.split * w.tw;
     const Pieces pc = pieces<PAIRS, F>(a, l);
     const float mean = 1.0f / a.D;
-    for (int j = threadIdx.x; j < a.D; j += kThreads) gains[j] = global_in<float>(hd.gain)[j];
+    if (hd.H > 0)                                      // a descriptor without heads need not have a gain
+        for (int j = threadIdx.x; j < a.D; j += kThreads) gains[j] = global_in<float>(hd.gain)[j];
     __syncthreads();
     Row<0, PAIRS, F> acc = {};
     Turn<PAIRS> turn;

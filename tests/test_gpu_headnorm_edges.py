@@ -1,0 +1,39 @@
+"""Norms of queries and keys with the rotation: calls at the edges of what the entry points take."""
+import pytest
+import torch
+
+from paper_2009_03106_amd import dpclip as dp
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+
+@pytest.mark.parametrize("empty", [0, 1], ids=["queries", "keys"])
+@pytest.mark.parametrize("B,T", [(2, 40), (700, 4)], ids=["chunks", "few"])
+@pytest.mark.parametrize("D", [64, 72, 33])
+def test_a_descriptor_without_heads_needs_no_addresses(empty, B, T, D):
+    """Its rows are zeros, the other one's results those of a call by itself."""
+    x, dy = (torch.randn(B, T, 3, D, device="cuda") for _ in range(2))
+    none = torch.empty(B, T, 0, D, device="cuda")
+    gain = 1 + 0.1 * torch.randn(D, device="cuda")
+    freqs = dp.rotary_freqs(32)
+    sq1, rows1, dx1 = dp.headnorm_sqnorm([(x, gain)], [dy], freqs=freqs)
+    y1, = dp.headnorm([(x, gain)], freqs=freqs)
+    order = (lambda a, b: [b, a]) if empty == 0 else (lambda a, b: [a, b])
+    out, dx, rows = torch.empty_like(x), torch.empty_like(x), [torch.full((B, D), 7.0, device="cuda") for _ in range(2)]
+    fwd = dp.head_descs(order((x, gain), (none, gain)), order(out, none))
+    bwd = dp.head_descs(order((x, gain), (none, gain)), order(dx, none), order(dy, none), rows)
+    for d in (fwd, bwd):
+        d.arr[empty].x = d.arr[empty].gain = d.arr[empty].out = d.arr[empty].dy = None
+    dp.headnorm(None, freqs=freqs, descs=fwd)
+    sq, _, _ = dp.headnorm_sqnorm(None, None, freqs=freqs, descs=bwd)
+    assert torch.equal(out, y1) and bool((rows[empty] == 0).all())
+    assert torch.equal(dx, dx1[0])
+    # the chunks may be others, so that sums of the same terms are taken in another order: 88 half steps of float32 of the sum of
+    # magnitudes on each side, a term's at most |x r| and twice the largest number of dy's row
+    xh = x.double() * (x.double().square().mean(-1, keepdim=True) + 1e-6).rsqrt()
+    off = 2 * 88 * 2.0 ** -24 * (2 * dy.double().abs().amax(-1, keepdim=True) * xh.abs()).sum((1, 2))
+    g = rows1[0].double()
+    assert bool(((rows[1 - empty].double() - g).abs() <= off).all())
+    assert bool(((sq.double() - sq1.double()).abs() <= (2 * g.abs() * off + off.square()).sum(1) + 2.0 ** -22 * sq1).all())
