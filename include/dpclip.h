@@ -413,8 +413,10 @@ int dp_conv_rows_resident(int64_t B, int64_t H, int64_t W, int64_t C,
  *     norm   = sqrt( (accumulate ? norm^2 : 0) + sum_l sum_j x_l[j]^2 )
  *     out_l  = (accumulate ? out_l : 0) + 1 / max(1, norm / C) * x_l
  * Squares and sums are taken in 64 bits, so neither overflows nor vanishes for any
- * float32 input, and `norm` is rounded to float32 once.  A NaN or an infinity in
- * any tensor makes the norm NaN or infinite; the factor is then NaN or 0.
+ * float32 input, and `norm` is rounded to float32 once: one beyond float32's largest
+ * number is stored as infinite.  norm / C may be beyond it, and the factor below the
+ * smallest one.  A NaN or an infinity in any tensor makes the norm NaN or infinite;
+ * the factor is then NaN or 0.
  * The tensors of a call may differ in type and size. */
 typedef struct {
     const void* x;       /* device, n elements of `dtype` one after the other, aligned to one element; NULL if n == 0 */
@@ -435,12 +437,14 @@ dp_status dp_tensors_norm(const dp_tensor_desc* tensors, int64_t n_tensors, int 
 
 /* out_l = (accumulate ? out_l : 0) + 1 / max(1, norm / C) * x_l with a norm that is on
  * the device already (one that dp_tensors_norm has taken, or that several processes
- * have added up).  C > 0. */
+ * have added up).  C > 0.  An infinite norm gives the factor 0, whatever made it infinite. */
 dp_status dp_tensors_clip(const dp_tensor_desc* tensors, int64_t n_tensors, const float* norm, float C,
                           int accumulate, void* workspace, size_t workspace_bytes, void* hip_stream);
 
 /* Both in one call: dp_tensors_norm without accumulating, then dp_tensors_clip, with
- * bit-identical results and fewer launches.  `accumulate` is that of the outputs. */
+ * bit-identical results and fewer launches; only that where finite tensors have a norm
+ * beyond float32's largest number, the factor is that of the norm in 64 bits here.
+ * `accumulate` is that of the outputs. */
 dp_status dp_tensors_norm_clip(const dp_tensor_desc* tensors, int64_t n_tensors, float C, int accumulate,
                                float* norm, float* tensor_norms,
                                void* workspace, size_t workspace_bytes, void* hip_stream);

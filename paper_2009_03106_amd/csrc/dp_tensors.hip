@@ -100,10 +100,10 @@ __device__ __forceinline__ void item_norm(const double* __restrict__ partial, in
     if ((threadIdx.x & (kWave - 1)) == 0) *out = (float)sqrt(s);
 }
 
-// workgroup 0: the norm; the others: the norms of four tensors each
+// workgroup 0: the norm, and in 64 bits for the launch that scales (wide, if not NULL); the others: the norms of four tensors each
 template <bool DIRECT>
 __global__ __launch_bounds__(kThreads) void k_tensors_fold(ItemTable t, const TensorItem* __restrict__ table, int n, int chunks, const double* __restrict__ partial,
-                                                           int accumulate, float* __restrict__ norm, float* __restrict__ tensor_norms) {
+                                                           int accumulate, float* __restrict__ norm, double* __restrict__ wide, float* __restrict__ tensor_norms) {
     __shared__ double red[4];
     const TensorItem* items = DIRECT ? t.items : table;
     if (blockIdx.x == 0) {
@@ -111,6 +111,7 @@ __global__ __launch_bounds__(kThreads) void k_tensors_fold(ItemTable t, const Te
         if (threadIdx.x == 0) {
             if (accumulate) { const double old = norm[0]; s += old * old; }
             norm[0] = (float)sqrt(s);
+            if (wide) wide[0] = sqrt(s);
         }
         return;
     }
@@ -118,10 +119,22 @@ __global__ __launch_bounds__(kThreads) void k_tensors_fold(ItemTable t, const Te
     if (i < n) item_norm(partial, items[i].first_chunk, i + 1 < n ? items[i + 1].first_chunk : chunks, tensor_norms + i);
 }
 
+// The factor 1 / max(1, norm / C), as a number that x is multiplied with first and one that follows.  norm / C is a float32 quotient
+// of the rounded norm while its reciprocal is a normal number (so a norm that was stored gives the same bits as the one it was
+// rounded from).  Beyond that it is taken in 64 bits, from the norm before its rounding where that is infinite, and where the
+// factor is below the normal numbers, x is scaled by 2^-126 first: what that rounds is below the result's own steps there.
+struct Factor { float first, then; };
+__device__ __forceinline__ Factor factor_of(double wide, float C) {
+    const float norm = (float)wide, m = norm / C;
+    if (m <= 0x1p126f) return Factor{1.0f, 1.0f / fmaxf(m, 1.0f)};
+    const double q = (double)C / (isinf(norm) ? wide : (double)norm), f = q > 1.0 ? 1.0 : q;       // NaN: lets it through
+    return f < 0x1p-126 ? Factor{0x1p-126f, (float)(f * 0x1p126)} : Factor{1.0f, (float)f};
+}
+
 // From the chunk's end, which the last-level cache got last.  Four pieces in flight, of 16 bytes where they are stored, next to each other
 // for neighbouring threads.  (340 MB of float32 in 2048 chunks: 176 us for the call, 192 with pieces of 32 bytes one at a time from the
 // beginning.  2 GB, most of it bf16: 1213 us, 1284 one at a time.)
-template <int DT, int ODT, bool PAST> __device__ __forceinline__ void scale(const void* x, void* out, int64_t begin, int64_t end, float f, bool accumulate, int tid) {
+template <int DT, int ODT, bool PAST> __device__ __forceinline__ void scale(const void* x, void* out, int64_t begin, int64_t end, Factor f, bool accumulate, int tid) {
     constexpr int V = ODT == 0 ? 4 : 8, U = 4;
     constexpr int64_t step = V * kThreads;
     const auto put = [&](int64_t k, float (&v)[V]) {
@@ -129,10 +142,10 @@ template <int DT, int ODT, bool PAST> __device__ __forceinline__ void scale(cons
             float o[V];
             load_piece<ODT>(out, k, o);
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] = o[j] + f * v[j];
+            for (int j = 0; j < V; ++j) v[j] = o[j] + f.then * (f.first * v[j]);
         } else {
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[j] *= f;
+            for (int j = 0; j < V; ++j) v[j] = f.then * (f.first * v[j]);
         }
         store_piece<ODT, PAST>(out, k, v);
     };
@@ -145,7 +158,7 @@ template <int DT, int ODT, bool PAST> __device__ __forceinline__ void scale(cons
             put(k, v);
         } else {
             for (; k < end; ++k) {
-                const float v = f * load_one<DT>(x, k);
+                const float v = f.then * (f.first * load_one<DT>(x, k));
                 store_one<ODT>(out, k, accumulate ? load_one<ODT>(out, k) + v : v);
             }
         }
@@ -164,8 +177,8 @@ template <int DT, int ODT, bool PAST> __device__ __forceinline__ void scale(cons
         put(k, v);
     }
 }
-template <bool PAST> __device__ __forceinline__ void chunk_scale(const TensorItem& it, int64_t begin, int64_t chunk, float f, bool accumulate, int tid) {
-    if (f == 1.0f && it.x == it.out && !accumulate) return;                // a factor of 1 leaves every value as it is
+template <bool PAST> __device__ __forceinline__ void chunk_scale(const TensorItem& it, int64_t begin, int64_t chunk, Factor f, bool accumulate, int tid) {
+    if (f.first == 1.0f && f.then == 1.0f && it.x == it.out && !accumulate) return;                // a factor of 1 leaves every value as it is
     const int64_t end = min(it.n, begin + chunk);
     switch (it.dt * 4 + it.odt) {
     case 0: scale<0, 0, PAST>(it.x, it.out, begin, end, f, accumulate, tid); break;
@@ -175,27 +188,23 @@ template <bool PAST> __device__ __forceinline__ void chunk_scale(const TensorIte
     default: scale<2, 2, PAST>(it.x, it.out, begin, end, f, false, tid); break;
     }
 }
-__device__ __forceinline__ float factor_of(float norm, float C) {
-    const float m = norm / C;
-    return 1.0f / (!(m <= 1.0f) ? m : 1.0f);           // the max lets a NaN norm through
-}
-
-// partial != nullptr: the norm is taken from the chunks' sums by every workgroup for itself, and written.  PAST: the outputs go past
+// partial != nullptr: the norm is taken from the chunks' sums by every workgroup for itself, and written.  wide != nullptr: it is there
+// in 64 bits.  Neither: norm is the caller's.  PAST: the outputs go past
 // the last-level cache, which they would not fit, and leave it to the inputs that are still to be read.
 template <bool DIRECT, bool PAST>
 __global__ __launch_bounds__(kThreads) void k_tensors_scale(ItemTable t, const TensorItem* __restrict__ table, int n, int64_t chunk, int chunks, int accumulate,
-                                                            const double* __restrict__ partial, float* __restrict__ norm, float* __restrict__ tensor_norms, float C) {
+                                                            const double* __restrict__ partial, const double* __restrict__ wide, float* __restrict__ norm, float* __restrict__ tensor_norms, float C) {
     __shared__ double red[4];
     const TensorItem* items = DIRECT ? t.items : table;
     const int c = chunks - 1 - blockIdx.x, i = find_item(items, n, c);        // the last chunks are in the last-level cache (2 GB: 1213 us, 1255 from the first one)
-    float total;
+    double total;
     if (partial) {
-        total = (float)sqrt(sum_partials(partial, chunks, red));
-        if (c == 0 && threadIdx.x == 0) norm[0] = total;
+        total = sqrt(sum_partials(partial, chunks, red));
+        if (c == 0 && threadIdx.x == 0) norm[0] = (float)total;
         if (tensor_norms && c == items[i].first_chunk && threadIdx.x < kWave)
             item_norm(partial, c, i + 1 < n ? items[i + 1].first_chunk : chunks, tensor_norms + i);
     } else {
-        total = norm[0];
+        total = wide ? wide[0] : norm[0];
     }
     chunk_scale<PAST>(items[i], (int64_t)(c - items[i].first_chunk) * chunk, chunk, factor_of(total, C), accumulate, threadIdx.x);
 }
@@ -226,21 +235,21 @@ __global__ __launch_bounds__(kFewThreads) void k_tensors_few(ItemTable t, int n,
         if (tid == 0 && c < chunks) partial[c] = (red[4 * group] + red[4 * group + 1]) + (red[4 * group + 2] + red[4 * group + 3]);
         __syncthreads();
     }
-    const float total = (float)sqrt(wave_sum_f64(lane < chunks ? partial[lane] : 0.0));
-    if (threadIdx.x == 0) norm[0] = total;
+    const double total = sqrt(wave_sum_f64(lane < chunks ? partial[lane] : 0.0));
+    if (threadIdx.x == 0) norm[0] = (float)total;
     if (tensor_norms && wave < n) {
         const int last = wave + 1 < n ? t.items[wave + 1].first_chunk : chunks, c = t.items[wave].first_chunk + lane;
         const double s = wave_sum_f64(c < last ? partial[c] : 0.0);
         if (lane == 0) tensor_norms[wave] = (float)sqrt(s);
     }
-    const float f = factor_of(total, C);
+    const Factor f = factor_of(total, C);
     for (int c = group; c < chunks; c += kGroups) {
         const int i = item_of(c);
         chunk_scale<false>(t.items[i], (int64_t)(c - t.items[i].first_chunk) * kTensorChunk, kTensorChunk, f, accumulate, tid);
     }
 }
 
-// Workspace: the table of items that do not fit the arguments, then the chunks' sums.
+// Workspace: the table of items that do not fit the arguments, then the chunks' sums, then the norm in 64 bits.
 size_t table_bytes(int64_t n) { return n > kDirectItems ? (size_t)n * sizeof(TensorItem) : 0; }
 
 struct Tables { ItemTable args; const TensorItem* table = nullptr; double* partial = nullptr; };
@@ -275,14 +284,14 @@ void squares(const Tables& t, int n, int64_t chunk, int chunks, hipStream_t st) 
     if (t.table) k_tensors_squares<false><<<chunks, kThreads, 0, st>>>(t.args, t.table, n, chunk, t.partial);
     else         k_tensors_squares<true><<<chunks, kThreads, 0, st>>>(t.args, nullptr, n, chunk, t.partial);
 }
-void fold(const Tables& t, int n, int chunks, bool accumulate, float* norm, float* tensor_norms, hipStream_t st) {
+void fold(const Tables& t, int n, int chunks, bool accumulate, float* norm, double* wide, float* tensor_norms, hipStream_t st) {
     const int grid = 1 + (tensor_norms ? ceil_div(n, kThreads / kWave) : 0);
-    if (t.table) k_tensors_fold<false><<<grid, kThreads, 0, st>>>(t.args, t.table, n, chunks, t.partial, accumulate, norm, tensor_norms);
-    else         k_tensors_fold<true><<<grid, kThreads, 0, st>>>(t.args, nullptr, n, chunks, t.partial, accumulate, norm, tensor_norms);
+    if (t.table) k_tensors_fold<false><<<grid, kThreads, 0, st>>>(t.args, t.table, n, chunks, t.partial, accumulate, norm, wide, tensor_norms);
+    else         k_tensors_fold<true><<<grid, kThreads, 0, st>>>(t.args, nullptr, n, chunks, t.partial, accumulate, norm, wide, tensor_norms);
 }
-void scaled(const Tables& t, int n, int64_t chunk, int chunks, bool accumulate, bool past, const double* partial, float* norm, float* tensor_norms, float C, hipStream_t st) {
+void scaled(const Tables& t, int n, int64_t chunk, int chunks, bool accumulate, bool past, const double* partial, const double* wide, float* norm, float* tensor_norms, float C, hipStream_t st) {
     const auto run = [&](auto kernel, const TensorItem* table) {
-        kernel<<<chunks, kThreads, 0, st>>>(t.args, table, n, chunk, chunks, accumulate, partial, norm, tensor_norms, C);
+        kernel<<<chunks, kThreads, 0, st>>>(t.args, table, n, chunk, chunks, accumulate, partial, wide, norm, tensor_norms, C);
     };
     if (t.table) run(past ? k_tensors_scale<false, true> : k_tensors_scale<false, false>, t.table);
     else         run(past ? k_tensors_scale<true, true> : k_tensors_scale<true, false>, nullptr);
@@ -308,14 +317,14 @@ hipError_t launch_tensors_norm(const TensorItem* items, int n, int64_t chunk, in
     const hipError_t e = place_items(items, n, ws, st, t);
     if (e != hipSuccess) return e;
     squares(t, n, chunk, chunks, st);
-    fold(t, n, chunks, accumulate, norm, tensor_norms, st);
+    fold(t, n, chunks, accumulate, norm, nullptr, tensor_norms, st);
     return hipGetLastError();
 }
 hipError_t launch_tensors_clip(const TensorItem* items, int n, int64_t chunk, int chunks, bool accumulate, const float* norm, float C, void* ws, hipStream_t st) {
     Tables t;
     const hipError_t e = place_items(items, n, ws, st, t);
     if (e != hipSuccess) return e;
-    scaled(t, n, chunk, chunks, accumulate, past_cache(items, n), nullptr, const_cast<float*>(norm), nullptr, C, st);
+    scaled(t, n, chunk, chunks, accumulate, past_cache(items, n), nullptr, nullptr, const_cast<float*>(norm), nullptr, C, st);
     return hipGetLastError();
 }
 hipError_t launch_tensors_norm_clip(const TensorItem* items, int n, int64_t chunk, int chunks, bool accumulate, float* norm, float* tensor_norms, float C, void* ws, hipStream_t st) {
@@ -328,10 +337,11 @@ hipError_t launch_tensors_norm_clip(const TensorItem* items, int n, int64_t chun
     }
     squares(t, n, chunk, chunks, st);
     if (chunks > kOwnFold) {
-        fold(t, n, chunks, false, norm, tensor_norms, st);
-        scaled(t, n, chunk, chunks, accumulate, past_cache(items, n), nullptr, norm, nullptr, C, st);
+        double* wide = t.partial + chunks;
+        fold(t, n, chunks, false, norm, wide, tensor_norms, st);
+        scaled(t, n, chunk, chunks, accumulate, past_cache(items, n), nullptr, wide, norm, nullptr, C, st);
     } else {
-        scaled(t, n, chunk, chunks, accumulate, past_cache(items, n), t.partial, norm, tensor_norms, C, st);
+        scaled(t, n, chunk, chunks, accumulate, past_cache(items, n), t.partial, nullptr, norm, tensor_norms, C, st);
     }
     return hipGetLastError();
 }
