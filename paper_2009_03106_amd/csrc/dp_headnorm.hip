@@ -103,11 +103,12 @@ template <int DT, bool PAIRS, Fill F> struct Row {
         store_some<DT, F, PAST>(p, at + c.a, c.na, lo);
         store_some<DT, F, PAST>(p, at + c.b, c.nb, hi);
     }
-    __device__ __forceinline__ void to_lds(const Pieces& c, float* row) const {
+    // to numbers of 32 or 64 bits, or (add) onto them
+    template <class S> __device__ __forceinline__ void to_lds(const Pieces& c, S* row, bool add) const {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            if (i < c.na) row[c.a + i] = lo[i];
-            if (i < c.nb) row[c.b + i] = hi[i];
+            if (i < c.na) row[c.a + i] = add ? row[c.a + i] + lo[i] : lo[i];
+            if (i < c.nb) row[c.b + i] = add ? row[c.b + i] + hi[i] : hi[i];
         }
     }
     __device__ __forceinline__ void from_lds(const Pieces& c, const float* row) {
@@ -236,7 +237,8 @@ __global__ __launch_bounds__(kThreads) void k_headnorm(HeadnormArgs a, Rows w) {
 }
 
 // Backward.  A workgroup has some tokens of an example and all of one descriptor's heads: the gains' gradients of a lane's columns
-// stay in its registers.  `split` of its waves share a token's heads.  The sums go to partial[example][chunk][D] of the descriptor.
+// stay in its registers, in float32.  `split` of its waves share a token's heads.  The sums go to partial[example][chunk][D] of the
+// descriptor.
 // (The next row's loads ahead of the present row's work made it slower, 89 us instead of 79 for 64 x 512 tokens of 12 + 12 heads of 64
 // bf16: the other waves' loads fill that time already, and the registers are theirs.)
 struct Back {
@@ -244,11 +246,21 @@ struct Back {
     int tokens, chunks;        // of a workgroup, of an example
     float* partial;
 };
-struct BackPlan { Back of[2]; int first; };            // workgroups from `first` on have the second descriptor's heads
+struct BackPlan {
+    Back of[2];
+    int first;                 // workgroups from here on have the second descriptor's heads
+    int64_t steps;             // rows that a group of lanes has, at most
+};
 
+// Where a wave has more than kChain steps, they join its sums in LDS every kChain steps, and those have 64 bits (S): however long the
+// sequence and many the heads, no more than kChain additions and six between the lanes follow each other in float32.  (Shorter ones
+// need no more than that anyway, and would pay for it: 33 x 1088 tokens of 2 + 1 heads of 128 bf16 25.1 us instead of 24.1.  Long ones
+// take as long as with one chain: 1 x 109226 of 5 + 1 heads of 128 bf16 132 us, 256 x 2048 of 32 + 8 3.23 ms.)
+constexpr int kChain = 64;
 // Tokens [t0, end) of example b by a workgroup: dx, and in sums[wave] the waves' shares of the gain's gradient.
-template <int DT, bool PAIRS, Fill F, bool PAST>
-__device__ __forceinline__ void back_rows(const HeadnormArgs& a, const HeadsArgs& hd, const Rows& w, int b, int64_t t0, int end, float* gains, float (*sums)[kMaxHeadDim]) {
+template <int DT, bool PAIRS, Fill F, bool PAST, class S>
+__device__ __forceinline__ void back_rows(const HeadnormArgs& a, const HeadsArgs& hd, const Rows& w, int b, int64_t t0, int end, float* gains, S (*sums)[kMaxHeadDim]) {
+    constexpr bool kLong = std::is_same_v<S, double>;
     const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l = lane & (w.L - 1), g = lane / w.L;
     const int part = wave % w.split, it0 = w.its * part / w.split, it1 = w.its * (part + 1) / w.split;
@@ -259,6 +271,17 @@ __device__ __forceinline__ void back_rows(const HeadnormArgs& a, const HeadsArgs
         for (int j = threadIdx.x; j < a.D; j += kThreads) gains[j] = global_in<float>(hd.gain)[j];
     __syncthreads();
     Row<0, PAIRS, F> acc = {};
+    int chain = 0;                                     // steps that acc has
+    bool some = false;                                 // whether sums[wave] has any
+    const auto gather = [&] {                          // the rows of a wave, in a fixed order, into its sums
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            for (int off = w.L; off < kWave; off <<= 1) {
+                acc.lo[i] += __shfl_xor(acc.lo[i], off, kWave);
+                acc.hi[i] += __shfl_xor(acc.hi[i], off, kWave);
+            }
+        if (g == 0) acc.to_lds(pc, sums[wave], kLong && some);
+    };
     Turn<PAIRS> turn;
     const int64_t x0 = b * hd.x_b, u0 = b * hd.dy_b, o0 = b * hd.o_b;
     for (int64_t n = t0 + wave / w.split * w.tw; n < end; n += step) {
@@ -266,6 +289,12 @@ __device__ __forceinline__ void back_rows(const HeadnormArgs& a, const HeadsArgs
         const bool here = t < end;
         turn.of(a, pc, !here ? 0 : a.positions ? a.positions[b * a.positions_b + t] : (int)t, here);
         for (int it = it0; it < it1; ++it) {
+            if (kLong && chain++ == kChain) {
+                gather();
+                acc = {};
+                some = true;
+                chain = 1;
+            }
             const int h = it * w.hw + (g & (w.hw - 1));
             const bool live = here && h < hd.H;
             Row<DT, PAIRS, F> x, u;
@@ -299,22 +328,15 @@ __device__ __forceinline__ void back_rows(const HeadnormArgs& a, const HeadsArgs
             if (live) x.template store<PAST>(pc, hd.out, o0 + t * hd.o_t + h * hd.o_h);
         }
     }
-    // the rows of a wave, then the waves, in a fixed order
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        for (int off = w.L; off < kWave; off <<= 1) {
-            acc.lo[i] += __shfl_xor(acc.lo[i], off, kWave);
-            acc.hi[i] += __shfl_xor(acc.hi[i], off, kWave);
-        }
-    if (g == 0) acc.to_lds(pc, sums[wave]);
+    gather();
     __syncthreads();
 }
 
 __device__ __forceinline__ int length_of(const HeadnormArgs& a, int b) { return a.lengths ? min(max(a.lengths[b], 0), a.T) : a.T; }
 
-template <int DT, bool PAIRS, Fill F, bool PAST>
+template <int DT, bool PAIRS, Fill F, bool PAST, class S>
 __global__ __launch_bounds__(kThreads, 3) void k_headnorm_back(HeadnormArgs a, BackPlan plan) {
-    __shared__ float sums[kThreads / kWave][kMaxHeadDim];
+    __shared__ S sums[kThreads / kWave][kMaxHeadDim];
     __shared__ __align__(16) float gains[kMaxHeadDim]; // not in registers, which decide how many waves there are
     const int which = (int)blockIdx.x >= plan.first;
     const Back& bk = plan.of[which];
@@ -323,10 +345,10 @@ __global__ __launch_bounds__(kThreads, 3) void k_headnorm_back(HeadnormArgs a, B
     const int end = (int)min(t0 + bk.tokens, (int64_t)length_of(a, b));
     back_rows<DT, PAIRS, F, PAST>(a, a.heads[which], bk.w, b, t0, end, gains, sums);
     for (int j = threadIdx.x; j < a.D; j += kThreads)
-        bk.partial[(int64_t)wg * a.D + j] = (sums[0][j] + sums[1][j]) + (sums[2][j] + sums[3][j]);
+        bk.partial[(int64_t)wg * a.D + j] = (float)((sums[0][j] + sums[1][j]) + (sums[2][j] + sums[3][j]));
 }
 
-// An example of few rows: a workgroup has all of them, and nothing is left to add up.
+// An example of few rows: a workgroup has all of them (at most kFewSteps for a wave), and nothing is left to add up.
 template <int DT, bool PAIRS, Fill F>
 __global__ __launch_bounds__(kThreads, 3) void k_headnorm_back_few(HeadnormArgs a, BackPlan plan, int accumulate, float* __restrict__ sqnorm) {
     __shared__ float sums[kThreads / kWave][kMaxHeadDim];
@@ -478,6 +500,7 @@ BackCost cut_back(const HeadnormArgs& a, int64_t per_wave, BackPlan& p) {
         k.chunks = ceil_div(a.T, k.tokens);
         c.workgroups += (int64_t)a.B * k.chunks;
         c.steps = std::max<int>(c.steps, ceil_div(k.tokens, granule) * its);
+        p.steps = std::max<int64_t>(i ? p.steps : 0, (int64_t)ceil_div(k.tokens, granule) * ceil_div(k.w.its, k.w.split));
     }
     return c;
 }
@@ -567,7 +590,10 @@ template <int DT> void backward_few(const HeadnormArgs& a, const BackPlan& p, bo
 }
 template <int DT> void backward(const HeadnormArgs& a, const BackPlan& p, hipStream_t st) {
     const int grid = a.B * (p.of[0].chunks + p.of[1].chunks);
-    by_layout<DT>(a, [&](auto pairs, auto fill, auto past) { k_headnorm_back<DT, pairs, fill, past><<<grid, kThreads, 0, st>>>(a, p); });
+    by_layout<DT>(a, [&](auto pairs, auto fill, auto past) {
+        if (p.steps > kChain) k_headnorm_back<DT, pairs, fill, past, double><<<grid, kThreads, 0, st>>>(a, p);
+        else                  k_headnorm_back<DT, pairs, fill, past, float><<<grid, kThreads, 0, st>>>(a, p);
+    });
 }
 
 }  // namespace

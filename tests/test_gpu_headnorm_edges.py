@@ -37,3 +37,24 @@ def test_a_descriptor_without_heads_needs_no_addresses(empty, B, T, D):
     g = rows1[0].double()
     assert bool(((rows[1 - empty].double() - g).abs() <= off).all())
     assert bool(((sq.double() - sq1.double()).abs() <= (2 * g.abs() * off + off.square()).sum(1) + 2.0 ** -22 * sq1).all())
+
+
+# one token of many heads (a chain of 2500 steps for each lane, were it not cut), and a batch that leaves one chunk to an example (600)
+@pytest.mark.parametrize("B,T,H", [(1, 1, 20000), (2400, 1200, 4)], ids=["heads", "tokens"])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_long_sums_of_a_gain(B, T, H, dtype):
+    """Equal rows: every addition of a column's chain is rounded the same way between two powers of two, so that errors add up instead of
+    cancelling.  A term u x r is off by 24 half steps of float32 (here: r, two products); with at most 64 additions one after the
+    other in float32, 6 between lanes, and a rounding of the chunk's sum and of the row: 24 + 64 + 6 + 2 = 96 of the sum."""
+    D = 512
+    x, gain = (1.0 + torch.arange(D, device="cuda") / D).to(dtype), torch.ones(D, device="cuda")
+    dy = (1.0 + torch.arange(D, device="cuda") / 397).to(dtype)
+    shape = (B, T, H, D)
+    dx = torch.empty(shape, device="cuda", dtype=dtype)
+    sq, (rows,), _ = dp.headnorm_sqnorm([(x.expand(shape), gain)], [dy.expand(shape)], outs=[dx], eps=1e-6)
+    want = dy.double() * x.double() / (x.double().square().mean() + 1e-6) ** 0.5 * (T * H)
+    off = (rows.double() - want).abs() / want * 2.0 ** 24
+    assert float(off.max()) <= 96, float(off.max())
+    assert torch.equal(rows, rows[:1].expand_as(rows))
+    s = want.square().sum()
+    assert float((sq.double() - s).abs().max()) <= 2 * 97 * 2.0 ** -24 * float(s)
