@@ -485,8 +485,8 @@ dp_status dp_posbias_add(const dp_posbias_desc* desc, const void* scores, const 
                          void* out, void* hip_stream);
 
 /* rows as above, and sqnorm[b] = (accumulate ? sqnorm[b] : 0) + ||rows[b]||^2.  The clipped sum of the rows is
- * dp_clipped_bias_grad(rows, clip, B, n_buckets * H, ...).  Up to eight neighbours
- * of a diagonal are added in float32, everything else in 64 bits.
+ * dp_clipped_bias_grad(rows, clip, B, n_buckets * H, ...).  Sums are taken in 64 bits
+ * (of 16-bit types up to eight neighbours of a diagonal in float32) and rounded once.
  *   dS         device, `dtype`, aligned to one element; the strides o_* are not looked at
  *   rows       device float32[B, n_buckets, H], written
  *   sqnorm     device float32[B]
@@ -503,9 +503,9 @@ size_t dp_posbias_workspace_bytes(int64_t B, int64_t H, int64_t Tq, int64_t Tk);
  * R(p) turns the pairs of the first `rot` numbers by the angles p freqs[j], p the token's
  * position; the numbers behind them stay.  Pairs are (j, j + rot / 2) or neighbours
  * (2 j, 2 j + 1).  Angles are taken in 64 bits, everything else in float32, y is
- * rounded once.  gain_rows below are added in float32 over at most 64 terms and a
- * wave's lanes, and in 64 bits beyond them.  dp_headnorm_sqnorm is the backward
- * pass: with u = R(p)^T dy,
+ * rounded once.  gain_rows below are added in float32 over at most 64 terms, a wave's
+ * lanes and four waves, and in 64 bits beyond them.  dp_headnorm_sqnorm is the
+ * backward pass: with u = R(p)^T dy,
  *     dx              = r (u (*) w - x r mean(u (*) w (*) x r)),
  *     gain_rows[i, :] = sum over example i's tokens and heads of u (*) x r,
  * the per-example gradient of the gain (the sum over the positions and heads that

@@ -149,7 +149,9 @@ AddTiles plan_add(int64_t BH, int Tq, int Tk) {
 // A lane adds up blocks of 8 queries x 8 keys along a diagonal of blocks: block (rb, rb + m) for one m and rb = r0, r0 + 1, ...
 // All of them have their elements on the same 15 diagonals, k - q = 8 m + e with -7 <= e <= 7, so the sums stay in the lane's
 // registers, and a group of LC lanes with neighbouring m reads LC pieces of 16 bytes (8 of float32: 32) next to each other
-// of every query.  The diagonal of a block is added in float32 (at most 8 elements), the blocks in 64 bits.
+// of every query.  Everything is added in 64 bits; only the diagonal of a block of 16-bit elements (at most 8 of them) in float32, whose
+// roundings are 2^-13 of the elements' own or less (in 64 bits 64 x 12 x 512 x 512 bf16 take 88 us instead of 86, 45 x 12 x 514 x 514 95
+// instead of 84).
 // 64 x 12 x 512 x 512 bf16: 88 us (4.6 TB/s; a copy of 4 GiB reaches 4.8).  A thread per diagonal, one element after the other in 64
 // bits, took 2950 us.
 struct Walk {
@@ -277,8 +279,14 @@ __global__ __launch_bounds__(kThreads, 3) void k_posbias_walk(PosbiasArgs a, con
             // no live element: left of the first key, behind the last one, all keys behind the queries
             if (rb + m < 0 || nk <= 0 || (a.causal && (int64_t)k0 - (q0 + 7) > w.start)) continue;
             float d[15];
+            if constexpr (DT != 0) {
 #pragma unroll
-            for (int e = 0; e < 15; ++e) d[e] = 0.f;
+                for (int e = 0; e < 15; ++e) d[e] = 0.f;
+            }
+            const auto add = [&](int e, float v) {
+                if constexpr (DT == 0) acc[e] += v;
+                else                   d[e] += v;
+            };
             if (narrow) {                              // rows shorter than a piece
                 for (int i = 0; i < nq; ++i) {
                     float v[8];
@@ -287,7 +295,7 @@ __global__ __launch_bounds__(kThreads, 3) void k_posbias_walk(PosbiasArgs a, con
                     for (int y = 0; y < 8; ++y)
                         if (y == i)
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) d[7 + j - y] += v[j];
+                            for (int j = 0; j < 8; ++j) add(7 + j - y, v[j]);
                 }
             } else {
                 // 128 bytes at once, all of them within the tensor: the last keys' pieces begin `over` earlier, queries behind the
@@ -307,7 +315,7 @@ __global__ __launch_bounds__(kThreads, 3) void k_posbias_walk(PosbiasArgs a, con
                             float v[8];
                             widen8<DT>(r[i], v);
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) d[7 + j - i0 - i] += v[j];
+                            for (int j = 0; j < 8; ++j) add(7 + j - i0 - i, v[j]);
                         }
                     } else {
 #pragma unroll
@@ -324,13 +332,21 @@ __global__ __launch_bounds__(kThreads, 3) void k_posbias_walk(PosbiasArgs a, con
 #pragma unroll
                                 for (int j = 0; j < 7; ++j) v[j] = last ? v[j + 1] : v[j];
 #pragma unroll
-                            for (int j = 0; j < 8; ++j) d[7 + j - i0 - i] += j < nk && i0 + i < nq ? v[j] : 0.f;
+                            for (int j = 0; j < 8; ++j) add(7 + j - i0 - i, j < nk && i0 + i < nq ? v[j] : 0.f);
+                            // a row's additions before the next one's selects: without this they take 10 registers more, and with
+                            // them a fourth of the waves (300 x 12 x 64 x 64: 38 us instead of 33)
+                            if constexpr (DT == 0) {
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) asm volatile("" : "+v"(acc[7 + j - i0 - i]));
+                            }
                         }
                     }
                 }
             }
+            if constexpr (DT != 0) {
 #pragma unroll
-            for (int e = 0; e < 15; ++e) acc[e] += d[e];
+                for (int e = 0; e < 15; ++e) acc[e] += d[e];
+            }
         }
     }
     // lane li's diagonals are slots 8 li ... 8 li + 14 of its group: the upper seven are the next lane's too

@@ -1,0 +1,50 @@
+"""Sums of the relative position bias's gradient, as close as their types allow.
+
+float32 elements are added in 64 bits: a row is off by one rounding to float32, 2^-24 of it, and by what 64-bit sums of n elements
+lose, n 2^-53 of the sum of magnitudes.  16-bit elements: at most 8 additions in float32, 8 * 2^-24 of the sum of magnitudes more.  The norm
+is that of the rows as they are written, in 64 bits and rounded once: 2^-24 of it."""
+import pytest
+import torch
+
+from paper_2009_03106_amd import dpclip as dp
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+SHAPES = [(1, 1, 1, 1), (2, 3, 9, 6), (2, 3, 63, 65), (3, 5, 197, 197), (1, 4, 530, 1100), (2, 2, 512, 512), (40, 17, 5, 6), (300, 2, 64, 64)]
+
+
+def exact(dS, buckets, nb, causal):
+    """Rows and sums of magnitudes in 64 bits, a diagonal at a time."""
+    B, H, Tq, Tk = dS.shape
+    reach = buckets.numel() // 2
+    flat = torch.nn.functional.pad(dS.double().flip(2), (0, Tq)).view(B, H, -1)[..., :Tq * (Tk + Tq - 1)].view(B, H, Tq, Tk + Tq - 1)
+    d = torch.arange(1 - Tq, Tk, device="cuda")
+    j = buckets[d.clamp(-reach, reach) + reach].long()
+    if causal:
+        j = torch.where(d <= 0, j, nb)
+    member = (j.view(-1, 1) == torch.arange(nb, device="cuda")).double()
+    return [torch.matmul(z.sum(2), member).transpose(1, 2) for z in (flat, flat.abs())]
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=["f32", "bf16", "f16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("causal", [False, True], ids=["both", "causal"])
+@pytest.mark.parametrize("nb,reach", [(32, 128), (1024, 700)])
+def test_sums(dtype, shape, causal, nb, reach):
+    gen = torch.Generator(device="cuda").manual_seed(sum(shape))
+    p = torch.randn(shape, device="cuda", generator=gen).softmax(-1)
+    g = torch.randn(shape, device="cuda", generator=gen)
+    dS = (p * (g - (p * g).sum(-1, keepdim=True)) * 2.0 ** (torch.randint(-6, 7, shape[2:], device="cuda", generator=gen))).to(dtype)      # of many sizes
+    if reach == 700:
+        buckets = torch.randint(-1, nb + 1, (2 * reach + 1,), device="cuda", generator=gen, dtype=torch.int32)
+    else:
+        buckets = dp.relative_buckets(nb, reach, both=not causal)
+    rows, mags = exact(dS, buckets, nb, causal)
+    sq, r = dp.posbias_sqnorm(dS, buckets, nb, torch.full(shape[:1], 3.0, device="cuda"), accumulate=True, causal=causal)
+    bound = 2.0 ** -24 * rows.abs() + (shape[2] * shape[3] * 2.0 ** -52 + (0.0 if dtype == F32 else 8 * 2.0 ** -24)) * mags + 2.0 ** -149
+    err = (r.double() - rows).abs()
+    assert bool((err <= bound).all()), float((err / bound).max())
+    s = 3.0 + r.double().square().sum((1, 2))
+    assert bool(((sq.double() - s).abs() <= 2.0 ** -24 * (1 + 2.0 ** -20) * s).all())
