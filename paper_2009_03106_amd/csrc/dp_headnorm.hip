@@ -91,6 +91,40 @@ template <int DT, Fill F, bool PAST> __device__ __forceinline__ void store_some(
     }
 }
 
+// sine and cosine of position * freq.  The angle is taken in quarter turns and in 64 bits, without the nearest whole number of them:
+// what is left is at most an eighth of a turn, and the series below are exact to float32 there (the first terms left out:
+// x^11 / 11! < 2e-9, x^12 / 12! < 2e-10 for x up to pi / 4).  Added to 1.5 2^52, a number below 2^51 is rounded to a whole one, whose
+// last bits are the sum's.
+__device__ __forceinline__ void sincos_of(int position, double freq, float& s, float& c) {
+    const double quarters = (double)position * (freq * 0.63661977236758134308), big = 6755399441055744.0, sum = quarters + big;
+    const float x = (float)(quarters - (sum - big)) * 1.5707963f;
+    const int q = (int)__double_as_longlong(sum) & 3;
+    const float z = x * x;
+    const float sx = x + x * z * (-1.6666667e-1f + z * (8.3333333e-3f + z * (-1.9841270e-4f + z * 2.7557319e-6f)));
+    const float cx = 1.0f + z * (-0.5f + z * (4.1666667e-2f + z * (-1.3888889e-3f + z * (2.4801587e-5f + z * -2.7557319e-7f))));
+    s = q & 1 ? cx : sx;
+    c = q & 1 ? sx : cx;
+    if (q & 2) s = -s;
+    if (q == 1 || q == 2) c = -c;
+}
+
+// the turn of each pair of a lane; those behind the rotated ones do not turn
+template <bool PAIRS> struct Turn {
+    float s[8], c[8];
+    int a, b;                  // PAIRS: how many pairs of each piece turn; halves: whether the lane's do
+    __device__ __forceinline__ void of(const HeadnormArgs& h, const Pieces& p, int position, bool live) {
+        a = PAIRS ? (h.rot - p.a) / 2 : p.a < h.rot / 2;
+        b = (h.rot - p.b) / 2;
+#pragma unroll
+        for (int v = 0; v < 8; ++v) {
+            s[v] = 0.f;
+            c[v] = 1.f;
+            const int j = !PAIRS ? p.a + v : v < 4 ? p.a / 2 + v : p.b / 2 + v - 4;
+            if (live && j < h.rot / 2) sincos_of(position, h.freqs[j], s[v], c[v]);
+        }
+    }
+};
+
 template <int DT, bool PAIRS, Fill F> struct Row {
     float lo[8], hi[8];        // (lo[i], hi[i]) turn together; PAIRS: neighbours within lo, and within hi
 
@@ -129,50 +163,20 @@ template <int DT, bool PAIRS, Fill F> struct Row {
             }
         }
     }
-    // the pairs, by the angles whose sines and cosines these are (sign -1: back)
-    __device__ __forceinline__ void rotate(const float (&s)[8], const float (&c)[8], float sign) {
-        const auto one = [&](float& x, float& y, int k) {
-            const float sk = sign * s[k], t = x * c[k] - y * sk;
-            y = x * sk + y * c[k];
-            x = t;
+    // The pairs that turn, by the angles whose sines and cosines these are (sign -1: back).  Numbers behind them are left alone: through a
+    // sine of 0 an infinite one would become its neighbour's NaN.
+    __device__ __forceinline__ void rotate(const Turn<PAIRS>& t, float sign) {
+        const auto one = [&](float& x, float& y, int k, bool turns) {
+            const float sk = sign * t.s[k], u = x * t.c[k] - y * sk, v = x * sk + y * t.c[k];
+            x = turns ? u : x;
+            y = turns ? v : y;
         };
         if constexpr (PAIRS) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) { one(lo[2 * i], lo[2 * i + 1], i); one(hi[2 * i], hi[2 * i + 1], 4 + i); }
-        } else {
+            for (int i = 0; i < 4; ++i) { one(lo[2 * i], lo[2 * i + 1], i, i < t.a); one(hi[2 * i], hi[2 * i + 1], 4 + i, i < t.b); }
+        } else if (t.a) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) one(lo[i], hi[i], i);
-        }
-    }
-};
-
-// sine and cosine of position * freq.  The angle is taken in quarter turns and in 64 bits, without the nearest whole number of them:
-// what is left is at most an eighth of a turn, and the series below are exact to float32 there (the first terms left out:
-// x^11 / 11! < 2e-9, x^12 / 12! < 2e-10 for x up to pi / 4).  Added to 1.5 2^52, a number below 2^51 is rounded to a whole one, whose
-// last bits are the sum's.
-__device__ __forceinline__ void sincos_of(int position, double freq, float& s, float& c) {
-    const double quarters = (double)position * (freq * 0.63661977236758134308), big = 6755399441055744.0, sum = quarters + big;
-    const float x = (float)(quarters - (sum - big)) * 1.5707963f;
-    const int q = (int)__double_as_longlong(sum) & 3;
-    const float z = x * x;
-    const float sx = x + x * z * (-1.6666667e-1f + z * (8.3333333e-3f + z * (-1.9841270e-4f + z * 2.7557319e-6f)));
-    const float cx = 1.0f + z * (-0.5f + z * (4.1666667e-2f + z * (-1.3888889e-3f + z * (2.4801587e-5f + z * -2.7557319e-7f))));
-    s = q & 1 ? cx : sx;
-    c = q & 1 ? sx : cx;
-    if (q & 2) s = -s;
-    if (q == 1 || q == 2) c = -c;
-}
-
-// the turn of each pair of a lane; those behind the rotated ones do not turn
-template <bool PAIRS> struct Turn {
-    float s[8], c[8];
-    __device__ __forceinline__ void of(const HeadnormArgs& a, const Pieces& p, int position, bool live) {
-#pragma unroll
-        for (int v = 0; v < 8; ++v) {
-            s[v] = 0.f;
-            c[v] = 1.f;
-            const int j = !PAIRS ? p.a + v : v < 4 ? p.a / 2 + v : p.b / 2 + v - 4;
-            if (live && j < a.rot / 2) sincos_of(position, a.freqs[j], s[v], c[v]);
+            for (int i = 0; i < 8; ++i) one(lo[i], hi[i], i, true);
         }
     }
 };
@@ -229,7 +233,7 @@ __global__ __launch_bounds__(kThreads) void k_headnorm(HeadnormArgs a, Rows w) {
                     x.lo[i] *= r * gain.lo[i];
                     x.hi[i] *= r * gain.hi[i];
                 }
-                x.rotate(turn.s, turn.c, 1.0f);
+                x.rotate(turn, 1.0f);
                 if (live) x.template store<PAST>(pc, hd.out, out + h * hd.o_h);
             }
         }
@@ -304,7 +308,7 @@ __device__ __forceinline__ void back_rows(const HeadnormArgs& a, const HeadsArgs
 #pragma unroll
             for (int i = 0; i < 8; ++i) sq += x.lo[i] * x.lo[i] + x.hi[i] * x.hi[i];
             const float r = rsqrtf(row_sum(sq, w.L) * mean + a.eps);
-            u.rotate(turn.s, turn.c, -1.0f);
+            u.rotate(turn, -1.0f);
             Row<0, PAIRS, F> gain;
             asm volatile("" ::: "memory");             // else the reads move out of the loops, and into registers
             gain.from_lds(pc, gains);

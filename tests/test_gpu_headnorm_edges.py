@@ -58,3 +58,31 @@ def test_long_sums_of_a_gain(B, T, H, dtype):
     assert torch.equal(rows, rows[:1].expand_as(rows))
     s = want.square().sum()
     assert float((sq.double() - s).abs().max()) <= 2 * 97 * 2.0 ** -24 * float(s)
+
+
+def only(x, column):
+    """Whether of the last dimension's columns just this one is not finite."""
+    bad = (~x.isfinite()).flatten(0, -2).any(0)
+    return bad.nonzero().flatten().tolist() == [column]
+
+
+@pytest.mark.parametrize("pairs", [False, True], ids=["halves", "pairs"])
+@pytest.mark.parametrize("D,rot,column", [(64, 32, 40), (64, 32, 57), (64, 0, 9), (80, 32, 79), (72, 24, 30), (33, 10, 11), (110, 54, 54), (128, 8, 9), (50, 20, 49)])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_what_does_not_turn_keeps_to_its_column(pairs, D, rot, column, dtype):
+    """An infinite gradient, or gain, of a number behind the ones that turn is no other column's."""
+    gen = torch.Generator(device="cuda").manual_seed(D)
+    x, dy = (torch.randn(2, 7, 3, D, device="cuda", generator=gen).to(dtype) for _ in range(2))
+    gain = 1 + 0.1 * torch.randn(D, device="cuda", generator=gen)
+    freqs = dp.rotary_freqs(rot) if rot else None
+    _, (want,), _ = dp.headnorm_sqnorm([(x, gain)], [dy], freqs=freqs, pairs=pairs)
+    before, = dp.headnorm([(x, gain)], freqs=freqs, pairs=pairs)
+    dy[1, 3, 2, column] = float("inf")
+    sq, (rows,), _ = dp.headnorm_sqnorm([(x, gain)], [dy], freqs=freqs, pairs=pairs)
+    assert torch.equal(rows[0], want[0]) and sq[0].isfinite() and sq[1].isinf()
+    assert only(rows[1:], column) and rows[1, column].isinf()
+    others = [j for j in range(D) if j != column]
+    assert torch.equal(rows[:, others], want[:, others])
+    gain[column] = float("inf")
+    y, = dp.headnorm([(x, gain)], freqs=freqs, pairs=pairs)
+    assert only(y, column) and bool(y[..., column].isinf().all()) and torch.equal(y[..., others], before[..., others])
