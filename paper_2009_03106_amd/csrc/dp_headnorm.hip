@@ -146,10 +146,10 @@ template <int DT, bool PAIRS, Fill F> struct Row {
         }
     }
     __device__ __forceinline__ void from_lds(const Pieces& c, const float* row) {
-        if constexpr (F != kAny) {                     // on 16 bytes; where there is none, something of the row, which meets zeros only
-            const float4* p = reinterpret_cast<const float4*>(row + (c.na ? c.a : 0));
-            const float4* q = reinterpret_cast<const float4*>(row + (c.nb ? c.b : 0));
-            const float4 f[4] = {p[0], p[F == kWhole || c.na > 4], q[0], q[F == kWhole || c.nb > 4]};
+        if constexpr (F != kAny) {                     // on 16 bytes; where there is none, the zeros behind the longest row
+            const auto at = [&](int column, bool there) { return reinterpret_cast<const float4*>(row + (there ? column : kMaxHeadDim)); };
+            const float4 *p = at(c.a, c.na), *q = at(c.b, c.nb);
+            const float4 f[4] = {p[0], F == kWhole ? p[1] : *at(c.a + 4, c.na > 4), q[0], F == kWhole ? q[1] : *at(c.b + 4, c.nb > 4)};
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 lo[4 * i] = f[i].x; lo[4 * i + 1] = f[i].y; lo[4 * i + 2] = f[i].z; lo[4 * i + 3] = f[i].w;
@@ -261,6 +261,7 @@ struct BackPlan {
 // need no more than that anyway, and would pay for it: 33 x 1088 tokens of 2 + 1 heads of 128 bf16 25.1 us instead of 24.1.  Long ones
 // take as long as with one chain: 1 x 109226 of 5 + 1 heads of 128 bf16 132 us, 256 x 2048 of 32 + 8 3.23 ms.)
 constexpr int kChain = 64;
+constexpr int kZeros = 8;                              // behind the gains in LDS
 // Tokens [t0, end) of example b by a workgroup: dx, and in sums[wave] the waves' shares of the gain's gradient.
 template <int DT, bool PAIRS, Fill F, bool PAST, class S>
 __device__ __forceinline__ void back_rows(const HeadnormArgs& a, const HeadsArgs& hd, const Rows& w, int b, int64_t t0, int end, float* gains, S (*sums)[kMaxHeadDim]) {
@@ -273,6 +274,7 @@ __device__ __forceinline__ void back_rows(const HeadnormArgs& a, const HeadsArgs
     const float mean = 1.0f / a.D;
     if (hd.H > 0)                                      // a descriptor without heads need not have a gain
         for (int j = threadIdx.x; j < a.D; j += kThreads) gains[j] = global_in<float>(hd.gain)[j];
+    if (threadIdx.x < kZeros) gains[kMaxHeadDim + threadIdx.x] = 0.f;
     __syncthreads();
     Row<0, PAIRS, F> acc = {};
     int chain = 0;                                     // steps that acc has
@@ -341,7 +343,7 @@ __device__ __forceinline__ int length_of(const HeadnormArgs& a, int b) { return 
 template <int DT, bool PAIRS, Fill F, bool PAST, class S>
 __global__ __launch_bounds__(kThreads, 3) void k_headnorm_back(HeadnormArgs a, BackPlan plan) {
     __shared__ S sums[kThreads / kWave][kMaxHeadDim];
-    __shared__ __align__(16) float gains[kMaxHeadDim]; // not in registers, which decide how many waves there are
+    __shared__ __align__(16) float gains[kMaxHeadDim + kZeros]; // not in registers, which decide how many waves there are
     const int which = (int)blockIdx.x >= plan.first;
     const Back& bk = plan.of[which];
     const int wg = blockIdx.x - (which ? plan.first : 0), b = wg / bk.chunks;
@@ -356,7 +358,7 @@ __global__ __launch_bounds__(kThreads, 3) void k_headnorm_back(HeadnormArgs a, B
 template <int DT, bool PAIRS, Fill F>
 __global__ __launch_bounds__(kThreads, 3) void k_headnorm_back_few(HeadnormArgs a, BackPlan plan, int accumulate, float* __restrict__ sqnorm) {
     __shared__ float sums[kThreads / kWave][kMaxHeadDim];
-    __shared__ __align__(16) float gains[kMaxHeadDim];
+    __shared__ __align__(16) float gains[kMaxHeadDim + kZeros];
     __shared__ double red[kThreads / kWave];
     const int b = blockIdx.x, end = length_of(a, b);
     double sq = 0.0;

@@ -86,3 +86,19 @@ def test_what_does_not_turn_keeps_to_its_column(pairs, D, rot, column, dtype):
     gain[column] = float("inf")
     y, = dp.headnorm([(x, gain)], freqs=freqs, pairs=pairs)
     assert only(y, column) and bool(y[..., column].isinf().all()) and torch.equal(y[..., others], before[..., others])
+
+
+@pytest.mark.parametrize("D,rot", [(64, 64), (80, 80), (80, 48), (72, 72), (100, 48), (36, 0), (33, 32), (176, 96)])
+@pytest.mark.parametrize("pairs", [False, True], ids=["halves", "pairs"])
+@pytest.mark.parametrize("B", [2, 500], ids=["chunks", "few"])
+@pytest.mark.parametrize("last", [False, True])
+def test_an_infinite_gain_meets_its_row_only(D, rot, pairs, B, last):
+    """dx = r (u w - x r mean(u w x r)): the mean is infinite, and so is every column but the gain's own, where infinities may cancel."""
+    gen = torch.Generator(device="cuda").manual_seed(D)
+    x, dy = (torch.randn(B, 3, 3, D, device="cuda", generator=gen) for _ in range(2))
+    gain = torch.ones(D, device="cuda")
+    column = D - 1 if last else 0
+    gain[column] = float("inf")
+    _, _, (dx,) = dp.headnorm_sqnorm([(x, gain)], [dy], freqs=dp.rotary_freqs(rot) if rot else None, pairs=pairs)
+    others = torch.cat((dx[..., :column], dx[..., column + 1:]), -1)
+    assert bool(others.isinf().all()), int(others.isnan().sum())
