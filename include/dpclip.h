@@ -490,11 +490,13 @@ dp_status dp_posbias_add(const dp_posbias_desc* desc, const void* scores, const 
  *   dS         device, `dtype`, aligned to one element; the strides o_* are not looked at
  *   rows       device float32[B, n_buckets, H], written
  *   sqnorm     device float32[B]
- *   workspace  device scratch of at least dp_posbias_workspace_bytes(B, H, Tq, Tk) bytes, 16-byte aligned */
+ *   workspace  device scratch of at least dp_posbias_table_workspace_bytes(B, H, Tq, Tk, n_buckets) bytes, 16-byte aligned */
 dp_status dp_posbias_sqnorm(const dp_posbias_desc* desc, const void* dS, dp_dtype dtype, int accumulate,
                             float* sqnorm, float* rows, void* workspace, size_t workspace_bytes, void* hip_stream);
 
-/* Scratch bytes for dp_posbias_sqnorm; 0 for sizes that need none or that it refuses. */
+/* Scratch bytes for dp_posbias_sqnorm; 0 for sizes that need none or that it refuses.  Without a number of buckets:
+ * those of the largest table, 1024 buckets, which are enough for any. */
+size_t dp_posbias_table_workspace_bytes(int64_t B, int64_t H, int64_t Tq, int64_t Tk, int64_t n_buckets);
 size_t dp_posbias_workspace_bytes(int64_t B, int64_t H, int64_t Tq, int64_t Tk);
 
 /* Norms of queries and keys for each head, with the position rotation in the same

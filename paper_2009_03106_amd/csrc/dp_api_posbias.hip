@@ -32,9 +32,13 @@ PosbiasArgs args_of(const dp_posbias_desc& d) {
 
 extern "C" {
 
+size_t dp_posbias_table_workspace_bytes(int64_t B, int64_t H, int64_t Tq, int64_t Tk, int64_t n_buckets) {
+    if (B <= 0 || H <= 0 || Tq <= 0 || Tk <= 0 || n_buckets < 1 || n_buckets > kMaxBuckets || !posbias_fits(B, H, Tq, Tk)) return 0;
+    return posbias_ws_bytes((int)B, (int)H, (int)Tq, (int)Tk, (int)n_buckets);
+}
+
 size_t dp_posbias_workspace_bytes(int64_t B, int64_t H, int64_t Tq, int64_t Tk) {
-    if (B <= 0 || H <= 0 || Tq <= 0 || Tk <= 0 || !posbias_fits(B, H, Tq, Tk)) return 0;
-    return posbias_ws_bytes((int)B, (int)H, (int)Tq, (int)Tk);
+    return dp_posbias_table_workspace_bytes(B, H, Tq, Tk, kMaxBuckets);
 }
 
 dp_status dp_posbias_add(const dp_posbias_desc* desc, const void* scores, const float* table, dp_dtype dtype, void* out, void* hip_stream) {
@@ -68,7 +72,8 @@ dp_status dp_posbias_sqnorm(const dp_posbias_desc* desc, const void* dS, dp_dtyp
         return DP_OK;
     }
     if (!dS || !rows || !d.buckets || !element_aligned(dS, dtype)) return DP_ERR_INVALID_ARG;
-    if (!workspace || workspace_bytes < posbias_ws_bytes((int)d.B, (int)d.H, (int)d.Tq, (int)d.Tk) || ((uintptr_t)workspace & 15) != 0) return DP_ERR_WORKSPACE;
+    const size_t need = posbias_ws_bytes((int)d.B, (int)d.H, (int)d.Tq, (int)d.Tk, (int)d.n_buckets);
+    if (!workspace || workspace_bytes < need || ((uintptr_t)workspace & 15) != 0) return DP_ERR_WORKSPACE;
     const hipError_t e = launch_posbias_sqnorm(args_of(d), dS, (int)dtype, accumulate != 0, rows, sqnorm, workspace, st);
     return e == hipSuccess ? DP_OK : DP_ERR_HIP;
 }

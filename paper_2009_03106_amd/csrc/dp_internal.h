@@ -128,7 +128,7 @@ struct PosbiasArgs {
 constexpr int kMaxBuckets = 1024;
 constexpr int64_t kMaxLength = int64_t(1) << 20;       // queries, keys
 bool posbias_fits(int64_t B, int64_t H, int64_t Tq, int64_t Tk);       // what the launches below hold
-size_t posbias_ws_bytes(int B, int H, int Tq, int Tk);
+size_t posbias_ws_bytes(int B, int H, int Tq, int Tk, int n_buckets);
 hipError_t launch_posbias_add(const PosbiasArgs& a, const void* scores, const float* table, int dt, void* out, hipStream_t st);
 hipError_t launch_posbias_sqnorm(const PosbiasArgs& a, const void* dS, int dt, bool accumulate, float* rows, float* sqnorm, void* ws, hipStream_t st);
 

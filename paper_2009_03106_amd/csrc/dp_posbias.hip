@@ -474,11 +474,11 @@ bool posbias_fits(int64_t B, int64_t H, int64_t Tq, int64_t Tk) {
     return launch_holds(B * H * t.row_tiles * t.col_tiles, kThreads)
         && launch_holds(B, kFinishThreads) && launch_holds(B * H * most_wgs(B * H, (int)Tq, (int)Tk), kThreads);
 }
-// the sums of every workgroup, where a head has several; whether keys are left out is not known here
-size_t posbias_ws_bytes(int B, int H, int Tq, int Tk) {
+// a number for every bucket and workgroup, where a head has several of them; whether keys are left out is not known here
+size_t posbias_ws_bytes(int B, int H, int Tq, int Tk, int n_buckets) {
     const int64_t BH = (int64_t)B * H;
     const int64_t wgs = most_wgs(BH, Tq, Tk);
-    return wgs > 1 ? (size_t)BH * wgs * kMaxBuckets * sizeof(double) : 16;
+    return wgs > 1 ? ((size_t)BH * wgs * n_buckets * sizeof(double) + 15) / 16 * 16 : 16;
 }
 
 hipError_t launch_posbias_add(const PosbiasArgs& a, const void* scores, const float* table, int dt, void* out, hipStream_t st) {

@@ -27,7 +27,7 @@ EXPORTS = ("dp_layer_sqnorm", "dp_layer_sqnorm_static", "dp_layers_sqnorm", "dp_
            "dp_layers_clipped_grad_noise", "dp_layers_step", "dp_layers_clipped_workspace_bytes", "dp_clip_factors", "dp_clipped_grad", "dp_bias_sqnorm", "dp_clipped_bias_grad", "dp_layernorm_sqnorm",
            "dp_conv_sqnorm", "dp_conv_clipped_grad", "dp_conv_workspace_bytes", "dp_conv_rows_resident", "dp_add_noise", "dp_workspace_bytes", "dp_choose_path", "dp_status_string", "dp_philox_raw",
            "dp_clipped_grad_rounds_inputs", "dp_tensors_norm", "dp_tensors_clip", "dp_tensors_norm_clip", "dp_tensors_workspace_bytes",
-           "dp_posbias_add", "dp_posbias_sqnorm", "dp_posbias_workspace_bytes",
+           "dp_posbias_add", "dp_posbias_sqnorm", "dp_posbias_workspace_bytes", "dp_posbias_table_workspace_bytes",
            "dp_headnorm", "dp_headnorm_sqnorm", "dp_headnorm_workspace_bytes")
 
 # the measurement probes and plan queries of include/dpclip_probes.h
@@ -153,6 +153,8 @@ def load_library() -> ctypes.CDLL:
     lib.dp_posbias_sqnorm.restype = ci
     lib.dp_posbias_workspace_bytes.argtypes = [i64, i64, i64, i64]
     lib.dp_posbias_workspace_bytes.restype = sz
+    lib.dp_posbias_table_workspace_bytes.argtypes = [i64, i64, i64, i64, i64]
+    lib.dp_posbias_table_workspace_bytes.restype = sz
     lib.dp_headnorm.argtypes = [ctypes.POINTER(HeadnormDesc), ctypes.POINTER(HeadsDesc), i64, ci, vp]
     lib.dp_headnorm.restype = ci
     lib.dp_headnorm_sqnorm.argtypes = [ctypes.POINTER(HeadnormDesc), ctypes.POINTER(HeadsDesc), i64, ci, ci, vp, vp, sz, vp]
@@ -874,8 +876,10 @@ def posbias_add(scores: torch.Tensor, table: torch.Tensor, buckets: torch.Tensor
     return out
 
 
-def posbias_workspace_bytes(dS: torch.Tensor) -> int:
-    return int(load_library().dp_posbias_workspace_bytes(*dS.shape))
+def posbias_workspace_bytes(dS: torch.Tensor, n_buckets: Optional[int] = None) -> int:
+    """Scratch bytes of posbias_sqnorm for dS and a table of n_buckets; without a number, enough for any table."""
+    lib = load_library()
+    return int(lib.dp_posbias_workspace_bytes(*dS.shape) if n_buckets is None else lib.dp_posbias_table_workspace_bytes(*dS.shape, n_buckets))
 
 
 def posbias_sqnorm(dS: torch.Tensor, buckets: torch.Tensor, n_buckets: int, sqnorm: Optional[torch.Tensor] = None,
@@ -897,7 +901,7 @@ def posbias_sqnorm(dS: torch.Tensor, buckets: torch.Tensor, n_buckets: int, sqno
             sqnorm = torch.empty(B, dtype=torch.float32, device=dS.device)
         if rows is None:
             rows = torch.empty((B, n_buckets, H), dtype=torch.float32, device=dS.device)
-        ws = _workspace(lambda: posbias_workspace_bytes(dS), dS.device, workspace)
+        ws = _workspace(lambda: posbias_workspace_bytes(dS, n_buckets), dS.device, workspace)
     st = lib.dp_posbias_sqnorm(ctypes.byref(d), xp, _dtype_code(dS), int(bool(accumulate)), _f32(sqnorm, (B,), "sqnorm"),
                                _f32(rows, (B, n_buckets, H), "rows"), *_ws_args(ws), _queue(stream, dev))
     _check(st, "dp_posbias_sqnorm")

@@ -48,3 +48,17 @@ def test_sums(dtype, shape, causal, nb, reach):
     assert bool((err <= bound).all()), float((err / bound).max())
     s = 3.0 + r.double().square().sum((1, 2))
     assert bool(((sq.double() - s).abs() <= 2.0 ** -24 * (1 + 2.0 ** -20) * s).all())
+
+
+@pytest.mark.parametrize("shape,nb", [((64, 12, 128, 128), 32), ((3, 5, 300, 301), 7), ((1, 1, 2000, 1500), 33), ((2, 2, 64, 64), 1)], ids=str)
+def test_a_workspace_of_the_table_is_enough(shape, nb):
+    """Nothing behind it is written, and what stood in it does not matter."""
+    dS = torch.randn(shape, device="cuda").to(BF16)
+    buckets = torch.randint(0, nb, (257,), device="cuda", dtype=torch.int32)
+    sq, rows = dp.posbias_sqnorm(dS, buckets, nb, workspace=torch.zeros(dp.posbias_workspace_bytes(dS), dtype=torch.uint8, device="cuda"))
+    n = dp.posbias_workspace_bytes(dS, nb)
+    ws = torch.full((n + 4096,), 255, dtype=torch.uint8, device="cuda")
+    sq2, rows2 = dp.posbias_sqnorm(dS, buckets, nb, workspace=ws[:n])
+    assert torch.equal(sq, sq2) and torch.equal(rows, rows2) and bool((ws[n:] == 255).all())
+    sq3, rows3 = dp.posbias_sqnorm(dS, buckets, nb)
+    assert torch.equal(sq, sq3) and torch.equal(rows, rows3)
