@@ -686,6 +686,17 @@ def _made_on(stream: Optional[torch.cuda.Stream]):
     return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
 
 
+def _no_graph(name: str, *tensors) -> None:
+    """The forward calls record nothing for autograd, whose graph would end at their outputs without a word: like torch's own calls with
+    out=, they refuse inputs and outputs that it would follow."""
+    if torch.is_grad_enabled() and any(getattr(t, "requires_grad", False) for t in tensors):
+        raise RuntimeError(f"{name} records no gradients: call it under torch.no_grad(), or with detached tensors; {name.split('_')[0]}_sqnorm is its backward pass")
+
+
+# tells autograd that a tensor's memory has changed, for the graphs that saved it
+_changed = torch.autograd.graph.increment_version
+
+
 def _ws_args(ws: Optional[torch.Tensor]):
     return (None, 0) if ws is None else (_ptr(ws), ws.numel() * ws.element_size())
 
@@ -857,8 +868,10 @@ def posbias_add(scores: torch.Tensor, table: torch.Tensor, buckets: torch.Tensor
     """out[b, h, q, k] = scores[b, h, q, k] + table[bucket of k - q - q_start[b], h] via dp_posbias_add, in place without
     out.  scores and out: [B, H, Tq, Tk], any strides but for the keys'; table: float32 [n_buckets, H]; buckets: int32 of odd length,
     one for each distance from -reach to reach (relative_buckets makes the usual ones); q_start, q_lens, k_lens: int32 [B].
-    Queries from q_lens[b] on, keys from k_lens[b] on and with causal the keys behind the query are left as they are in out."""
+    Queries from q_lens[b] on, keys from k_lens[b] on and with causal the keys behind the query are left as they are in out.
+    Nothing is recorded for autograd: tensors that require gradients are refused unless gradients are switched off."""
     lib = load_library()
+    _no_graph("posbias_add", scores, table, out)
     xp = _inner(scores, 4, "scores")
     if out is None:
         out, op = scores, xp
@@ -873,6 +886,7 @@ def posbias_add(scores: torch.Tensor, table: torch.Tensor, buckets: torch.Tensor
     st = lib.dp_posbias_add(ctypes.byref(d), xp, _vec(table, torch.float32, table.numel(), "table"), _ELEMENT_CODES[scores.dtype], op,
                             _queue(stream, dev))
     _check(st, "dp_posbias_add")
+    _changed(out)
     return out
 
 
@@ -917,6 +931,7 @@ class HeadDescs(NamedTuple):
     dtype: int
     outs: list
     gain_rows: Optional[list]
+    followed: Optional[torch.Tensor]    # one of the inputs or outputs that autograd follows, if there is any
 
     def here(self) -> None:
         if self.device.index != torch._C._cuda_getDevice():
@@ -958,8 +973,9 @@ def head_descs(heads, outs, dys=None, gain_rows=None) -> HeadDescs:
         if any(t.device != x0.device for t in (x, *others)):
             raise ValueError("tensors must all be on one device")
         arr[i] = HeadsDesc(xp, s[0], s[1], s[2], H, _f32(gain, (D,), "gain"), op, o[0], o[1], o[2], gp, g[0], g[1], g[2], rp)
+    followed = next((t for t in (*(t for head in heads for t in head), *outs) if t.requires_grad), None)
     return HeadDescs(arr, x0.device, x0.shape[0], x0.shape[1], x0.shape[3], _dtype_code(x0), list(outs),
-                     None if gain_rows is None else list(gain_rows))
+                     None if gain_rows is None else list(gain_rows), followed)
 
 
 def _headnorm_desc(d: HeadDescs, freqs, positions, lengths, pairs, eps) -> HeadnormDesc:
@@ -986,19 +1002,25 @@ def headnorm(heads, outs=None, *, freqs: Optional[torch.Tensor] = None, position
     heads, outs: as in head_descs (outs made if None, with zeros where lengths leave tokens out); freqs: float64, None for no rotation
     (rotary_freqs makes the usual ones); positions: int32 [B, T] or [T], None for 0, 1, ...; pairs: neighbours turn together
     instead of the halves' numbers; lengths: int32 [B], tokens from there on are left as they are in outs.
-    descs: the result of head_descs(heads, outs), to skip rebuilding it on every call."""
+    descs: the result of head_descs(heads, outs), to skip rebuilding it on every call.
+    Nothing is recorded for autograd: tensors that require gradients are refused unless gradients are switched off."""
     lib = load_library()
     if descs is None:
+        heads = list(heads)
+        _no_graph("headnorm", *(t for head in heads for t in head), *(outs or ()))
         with _made_on(stream):
             if outs is None:
                 make = torch.empty if lengths is None else torch.zeros
                 outs = [make(x.shape, dtype=x.dtype, device=x.device) for x, _ in heads]
         descs = head_descs(heads, outs)
+    else:
+        _no_graph("headnorm", descs.followed)
     dev = _here(stream, freqs, positions, lengths)
     descs.here()
     d = _headnorm_desc(descs, freqs, positions, lengths, pairs, eps)
     st = lib.dp_headnorm(ctypes.byref(d), descs.arr, len(descs.arr), descs.dtype, _queue(stream, dev))
     _check(st, "dp_headnorm")
+    _changed(descs.outs)
     return descs.outs
 
 
