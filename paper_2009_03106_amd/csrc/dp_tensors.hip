@@ -270,7 +270,9 @@ hipError_t place_items(const TensorItem* items, int n, void* ws, hipStream_t st,
 }
 
 // Whether the outputs are larger than the last-level cache: nothing that reads them behind the call finds them there.
-// (340 MB of float32: 176 us past the cache, 212 through it; smaller outputs stay, for the optimizer step that reads them next.)
+// (340 MB of float32: 164 us past the cache, 194 through it; 600 MB of bf16 304 and 333.  In place of the inputs, or added to sums, it
+// makes no difference: 164 and 165, 253 and 252 for that float32, 329 and 330, 696 and 696 for that bf16.  Smaller outputs stay, for the
+// optimizer step that reads them next.)
 bool past_cache(const TensorItem* items, int n) {
     int64_t bytes = 0;
     for (int i = 0; i < n; ++i) bytes += items[i].n * (items[i].odt == 0 ? 4 : 2);
@@ -301,9 +303,11 @@ void scaled(const Tables& t, int n, int64_t chunk, int chunks, bool accumulate, 
 
 // Chunks of at least 4096 elements (two 16-byte pieces of float32 for every thread), and larger ones where that makes more than
 // 2048 of them (eight workgroups for each of the 256 compute units, and sums that every workgroup still adds up by itself: 31 million
-// float32 66 us, in smaller chunks and with a launch for the sums 72).  From 67 million elements on there are eight times as many:
-// the ends of the last ones matter less, and what the first pass reads last is then a part of the set, where the second one begins
-// (2 GB: 1093 us, 1213 in 2048 chunks, all of which are worked on at once).
+// float32 66 us, in smaller chunks and with a launch for the sums 72).  From 67 million elements on there are eight times as many, of
+// the smallest size at least: the ends of the last ones matter less, and of a set beyond the last-level cache what the first pass reads
+// last is then a part, where the second one begins (340 MB of float32 164 us, 171 in 2048 chunks, all of which are worked on at once; 2 GB of
+// bf16 1072 and 1095).  Of 16 bits that the cache still holds it is about even: 140 MB of bf16 72 us and 70, in place 72 and 70,
+// added to float32 sums 157 and 169; 250 MB 141 and 147, 117 and 116, 279 and 301.
 int64_t tensor_chunk_elems(int64_t total) {
     const int64_t unit = 8 * kThreads, most = total < (int64_t)kTensorChunk * kTensorChunksLarge ? kTensorChunks : kTensorChunksLarge;
     return std::max<int64_t>(kTensorChunk, (total / most + unit) / unit * unit);
