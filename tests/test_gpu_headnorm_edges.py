@@ -102,3 +102,14 @@ def test_an_infinite_gain_meets_its_row_only(D, rot, pairs, B, last):
     _, _, (dx,) = dp.headnorm_sqnorm([(x, gain)], [dy], freqs=dp.rotary_freqs(rot) if rot else None, pairs=pairs)
     others = torch.cat((dx[..., :column], dx[..., column + 1:]), -1)
     assert bool(others.isinf().all()), int(others.isnan().sum())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16], ids=["f32", "bf16", "f16"])
+@pytest.mark.parametrize("D,rot", [(64, 64), (72, 72), (100, 48), (110, 54), (33, 0), (16, 16)])
+@pytest.mark.parametrize("pairs", [False, True], ids=["halves", "pairs"])
+def test_sums_of_many_heads(dtype, D, rot, pairs):
+    """More rows for each lane than a chain of float32 has, of two descriptors with different numbers of them."""
+    from test_gpu_headnorm import check, full, make
+    lengths = torch.tensor([2, 1], dtype=torch.int32, device="cuda")
+    heads, dys = make(2, 2, (30000, 20), D, dtype, seed=D, lengths=lengths)
+    check(heads, dys, full(heads), full(heads), dp.rotary_freqs(rot) if rot else None, lengths=lengths, pairs=pairs)
