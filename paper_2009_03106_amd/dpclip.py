@@ -686,15 +686,17 @@ def _made_on(stream: Optional[torch.cuda.Stream]):
     return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
 
 
-def _no_graph(name: str, *tensors) -> None:
-    """The forward calls record nothing for autograd, whose graph would end at their outputs without a word: like torch's own calls with
-    out=, they refuse inputs and outputs that it would follow."""
-    if torch.is_grad_enabled() and any(getattr(t, "requires_grad", False) for t in tensors):
-        raise RuntimeError(f"{name} records no gradients: call it under torch.no_grad(), or with detached tensors; {name.split('_')[0]}_sqnorm is its backward pass")
+# The forward calls record nothing for autograd, whose graph would end at their outputs without a word: like torch's own calls with
+# out=, they refuse inputs and outputs that it would follow.
+_graphs_on = torch.is_grad_enabled
 
 
-# tells autograd that a tensor's memory has changed, for the graphs that saved it
-_changed = torch.autograd.graph.increment_version
+def _no_graph(name: str) -> RuntimeError:
+    return RuntimeError(f"{name} records no gradients: call it under torch.no_grad(), or with detached tensors; {name.split('_')[0]}_sqnorm is its backward pass")
+
+
+# tells autograd that the memory of a list of tensors has changed, for the graphs that saved them
+_changed = getattr(torch._C, "_increment_version", torch.autograd.graph.increment_version)
 
 
 def _ws_args(ws: Optional[torch.Tensor]):
@@ -849,10 +851,9 @@ def _inner(t: torch.Tensor, dims: int, name: str) -> int:
     return t.data_ptr()
 
 
-def _posbias_desc(x: torch.Tensor, out: Optional[torch.Tensor], buckets, n_buckets: int, q_start, q_lens, k_lens, causal) -> PosbiasDesc:
-    B, H, Tq, Tk = x.shape
-    s = x.stride()
-    o = s if out is None else out.stride()
+def _posbias_desc(shape, s, o, buckets, n_buckets: int, q_start, q_lens, k_lens, causal) -> PosbiasDesc:
+    """s, o: the strides of the scores and of the outputs."""
+    B, H, Tq, Tk = shape
     n = buckets.numel()
     if n % 2 == 0:
         raise ValueError("buckets must hold one for each distance from -reach to reach")
@@ -871,22 +872,25 @@ def posbias_add(scores: torch.Tensor, table: torch.Tensor, buckets: torch.Tensor
     Queries from q_lens[b] on, keys from k_lens[b] on and with causal the keys behind the query are left as they are in out.
     Nothing is recorded for autograd: tensors that require gradients are refused unless gradients are switched off."""
     lib = load_library()
-    _no_graph("posbias_add", scores, table, out)
-    xp = _inner(scores, 4, "scores")
+    if not isinstance(table, torch.Tensor):
+        raise ValueError("table must be [n_buckets, H]")
+    if _graphs_on() and (scores.requires_grad or table.requires_grad or (out is not None and out.requires_grad)):
+        raise _no_graph("posbias_add")
+    xp, shape, size = _inner(scores, 4, "scores"), scores.shape, table.shape
     if out is None:
         out, op = scores, xp
     else:
         op = _inner(out, 4, "out")
-        if out.shape != scores.shape or out.dtype is not scores.dtype:
+        if out.shape != shape or out.dtype is not scores.dtype:
             raise ValueError("out must have the shape and the dtype of scores")
-    if not isinstance(table, torch.Tensor) or table.dim() != 2 or table.shape[1] != scores.shape[1]:
+    if len(size) != 2 or size[1] != shape[1]:
         raise ValueError("table must be [n_buckets, H]")
     dev = _here(stream, scores, out, table, buckets, q_start, q_lens, k_lens)
-    d = _posbias_desc(scores, out, buckets, table.shape[0], q_start, q_lens, k_lens, causal)
+    d = _posbias_desc(shape, scores.stride(), out.stride(), buckets, size[0], q_start, q_lens, k_lens, causal)
     st = lib.dp_posbias_add(ctypes.byref(d), xp, _vec(table, torch.float32, table.numel(), "table"), _ELEMENT_CODES[scores.dtype], op,
                             _queue(stream, dev))
     _check(st, "dp_posbias_add")
-    _changed(out)
+    _changed([out])
     return out
 
 
@@ -909,7 +913,8 @@ def posbias_sqnorm(dS: torch.Tensor, buckets: torch.Tensor, n_buckets: int, sqno
     if sqnorm is None and accumulate:
         raise ValueError("accumulate needs an existing sqnorm tensor")
     dev = _here(stream, dS, sqnorm, rows, buckets, q_start, q_lens, k_lens, workspace)
-    d = _posbias_desc(dS, None, buckets, n_buckets, q_start, q_lens, k_lens, causal)
+    strides = dS.stride()
+    d = _posbias_desc(dS.shape, strides, strides, buckets, n_buckets, q_start, q_lens, k_lens, causal)
     with _made_on(stream):
         if sqnorm is None:
             sqnorm = torch.empty(B, dtype=torch.float32, device=dS.device)
@@ -931,7 +936,7 @@ class HeadDescs(NamedTuple):
     dtype: int
     outs: list
     gain_rows: Optional[list]
-    followed: Optional[torch.Tensor]    # one of the inputs or outputs that autograd follows, if there is any
+    followed: bool                  # whether autograd follows any of the inputs or outputs
 
     def here(self) -> None:
         if self.device.index != torch._C._cuda_getDevice():
@@ -973,7 +978,7 @@ def head_descs(heads, outs, dys=None, gain_rows=None) -> HeadDescs:
         if any(t.device != x0.device for t in (x, *others)):
             raise ValueError("tensors must all be on one device")
         arr[i] = HeadsDesc(xp, s[0], s[1], s[2], H, _f32(gain, (D,), "gain"), op, o[0], o[1], o[2], gp, g[0], g[1], g[2], rp)
-    followed = next((t for t in (*(t for head in heads for t in head), *outs) if t.requires_grad), None)
+    followed = any(t.requires_grad for t in (*(t for head in heads for t in head), *outs))
     return HeadDescs(arr, x0.device, x0.shape[0], x0.shape[1], x0.shape[3], _dtype_code(x0), list(outs),
                      None if gain_rows is None else list(gain_rows), followed)
 
@@ -986,10 +991,12 @@ def _headnorm_desc(d: HeadDescs, freqs, positions, lengths, pairs, eps) -> Headn
         rot = 2 * freqs.numel()
     pp, pb = None, 0
     if positions is not None:
-        if positions.shape not in ((d.T,), (d.B, d.T)):
-            raise ValueError(f"positions must be [{d.T}] or [{d.B}, {d.T}], got {tuple(positions.shape)}")
-        pb = d.T if positions.dim() == 2 else 0
-        pp = _vec(positions, torch.int32, positions.numel(), "positions")
+        shape = positions.shape
+        if shape == (d.B, d.T):
+            pb = d.T
+        elif shape != (d.T,):
+            raise ValueError(f"positions must be [{d.T}] or [{d.B}, {d.T}], got {tuple(shape)}")
+        pp = _vec(positions, torch.int32, d.B * d.T if pb else d.T, "positions")
     return HeadnormDesc(d.B, d.T, d.D, rot, int(bool(pairs)), float(eps), pp, pb, freqs.data_ptr() if rot else None,
                         _vec(lengths, torch.int32, d.B, "lengths"))
 
@@ -1007,16 +1014,18 @@ def headnorm(heads, outs=None, *, freqs: Optional[torch.Tensor] = None, position
     lib = load_library()
     if descs is None:
         heads = list(heads)
-        _no_graph("headnorm", *(t for head in heads for t in head), *(outs or ()))
+        if _graphs_on() and any(t.requires_grad for t in (*(t for head in heads for t in head), *(outs or ()))):
+            raise _no_graph("headnorm")
         with _made_on(stream):
             if outs is None:
                 make = torch.empty if lengths is None else torch.zeros
                 outs = [make(x.shape, dtype=x.dtype, device=x.device) for x, _ in heads]
         descs = head_descs(heads, outs)
-    else:
-        _no_graph("headnorm", descs.followed)
+    elif descs.followed and _graphs_on():
+        raise _no_graph("headnorm")
     dev = _here(stream, freqs, positions, lengths)
-    descs.here()
+    if descs.device.index != dev:
+        descs.here()
     d = _headnorm_desc(descs, freqs, positions, lengths, pairs, eps)
     st = lib.dp_headnorm(ctypes.byref(d), descs.arr, len(descs.arr), descs.dtype, _queue(stream, dev))
     _check(st, "dp_headnorm")
